@@ -18,6 +18,8 @@ MODE_DENSE, MODE_KV, MODE_O, MODE_BOTH = 0, 1, 2, 3
 FORM_SCORE_FIRST, FORM_SPLIT_Q, FORM_SPLIT_KV, FORM_SPLIT_OUT = 1, 2, 4, 8
 F32, BF16 = 0, 1
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
+ROPE_SCALE = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 
 
 class LayerConfig(C.Structure):
@@ -44,6 +46,19 @@ class BlockWeights(C.Structure):
 class StackWeights(C.Structure):
     _fields_ = [("emb", C.c_void_p), ("head", C.c_void_p), ("final_gain", C.c_void_p),
                 ("blocks_host", C.POINTER(BlockWeights))]
+
+
+class RopeConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rotary_dim", C.c_int32), ("theta", C.c_double), ("scaling", C.c_int32),
+                ("trained", C.c_int32), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("magnitude", C.c_double)]
+
+
+class RopeApply(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("tokens", C.c_int64), ("heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("transpose", C.c_int32),
+                ("pos_begin", C.c_int32), ("x_token", C.c_int64), ("x_head", C.c_int64), ("y_token", C.c_int64),
+                ("y_head", C.c_int64), ("table_positions", C.c_int64)]
 
 
 class DareError(RuntimeError):
@@ -102,6 +117,8 @@ def _load():
         "dare_select_compact": (C.c_int, [vp, C.c_int64, f32, vp, vp, vp, sz, vp]),
         "dare_select_compact_static_max_tokens": (C.c_int64, []),
         "dare_select_compact_static": (C.c_int, [vp, C.c_int64, f32, vp, vp, vp]),
+        "dare_rope_table": (C.c_int, [C.POINTER(RopeConfig), vp, C.c_int64, vp]),
+        "dare_rope": (C.c_int, [C.POINTER(RopeApply), vp, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -268,6 +285,14 @@ def dare_select_compact_static(scores_ptr, n_tokens, threshold, idx_ptr, count_p
     return _lib.dare_select_compact_static(scores_ptr, n_tokens, threshold, idx_ptr, count_ptr, stream)
 
 
+def dare_rope_table(cfg: RopeConfig, table_ptr, positions, stream=0) -> int:
+    return _lib.dare_rope_table(C.byref(cfg) if cfg is not None else None, table_ptr, positions, stream)
+
+
+def dare_rope(cfg: RopeApply, x_ptr, positions_ptr, table_ptr, y_ptr, status_ptr=None, stream=0) -> int:
+    return _lib.dare_rope(C.byref(cfg) if cfg is not None else None, x_ptr, positions_ptr, table_ptr, y_ptr, status_ptr, stream)
+
+
 def dare_kernel_slot_name(slot: int) -> str:
     return _lib.dare_kernel_slot_name(slot).decode()
 
@@ -324,6 +349,83 @@ def _current_stream(torch, device) -> int:
     if raw is None or device.index is None:
         return torch.cuda.current_stream(device).cuda_stream
     return raw(device.index)
+
+
+# Stand-alone operators on torch tensors: argument marshalling, outputs and workspaces from torch's allocator, the tensors' device
+# and its current stream.  `status`: an int32 CUDA tensor of one element that device-side problems are recorded in, or None.
+class _on_device:
+    """Makes the tensors' device the current one for a call (a no-op where it is)."""
+
+    def __init__(self, torch, device):
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _check(cond, what):
+    if not cond:
+        raise ValueError(what)
+
+
+def _dtype_of(torch, x):
+    _check(x.dtype in (torch.bfloat16, torch.float32), f"bf16 or float32 expected, not {x.dtype}")
+    return BF16 if x.dtype == torch.bfloat16 else F32
+
+
+def _same_device(x, *others):
+    _check(x.is_cuda, "CUDA tensors expected")
+    for t in others:
+        _check(t is None or t.device == x.device, "tensors on different devices")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def rope_table(positions, rotary_dim, theta, scaling=ROPE_SCALE["none"], factor=1.0, trained=0, low=1.0, high=32.0,
+               magnitude=1.0, device="cuda", out=None):
+    """-> float32 [positions, rotary_dim / 2, 2]: cosines and sines of dare_rope_table, for `rope`."""
+    import torch
+    if out is None:
+        out = torch.empty((positions, rotary_dim // 2, 2), dtype=torch.float32, device=device)
+    _check(out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.shape == (positions, rotary_dim // 2, 2),
+           "out: contiguous float32 CUDA tensor [positions, rotary_dim / 2, 2] expected")
+    cfg = RopeConfig(C.sizeof(RopeConfig), rotary_dim, theta, scaling, trained, factor, low, high, magnitude)
+    with _on_device(torch, out.device):
+        st = dare_rope_table(cfg, out.data_ptr(), positions, _current_stream(torch, out.device))
+    if st != OK:
+        raise DareError(st, "dare_rope_table")
+    return out
+
+
+def rope(x, table, positions=None, layout=ROPE_LAYOUT["half"], transpose=False, pos_begin=0, out=None, status=None):
+    """x [tokens, heads, head_dim] (any token and head strides) with its heads turned by the table's rows of `positions` (int32
+    [tokens]; None: pos_begin, pos_begin + 1, ...).  The table's width gives the part of the head that turns.  out may be x."""
+    import torch
+    dt = _dtype_of(torch, x)
+    _same_device(x, table, positions, out, status)
+    _check(x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1), "x: [tokens, heads, head_dim] with the head's elements side by side")
+    _check(table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous(),
+           "table: contiguous float32 [positions, rotary_dim / 2, 2] expected")
+    _check(positions is None or (positions.dtype == torch.int32 and positions.shape == x.shape[:1] and positions.is_contiguous()),
+           "positions: contiguous int32 [tokens] expected")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check(out.shape == x.shape and out.dtype == x.dtype and (out.stride(2) == 1 or x.shape[2] == 1), "out: as x")
+    cfg = RopeApply(C.sizeof(RopeApply), dt, x.shape[0], x.shape[1], x.shape[2], table.shape[1] * 2, layout, 1 if transpose else 0,
+                    pos_begin, x.stride(0), x.stride(1), out.stride(0), out.stride(1), table.shape[0])
+    with _on_device(torch, x.device):
+        st = dare_rope(cfg, x.data_ptr(), _ptr(positions), table.data_ptr(), out.data_ptr(), _ptr(status),
+                       _current_stream(torch, x.device))
+    if st != OK:
+        raise DareError(st, "dare_rope")
+    return out
 
 
 class Layer:

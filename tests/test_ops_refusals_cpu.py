@@ -1,0 +1,57 @@
+"""No-GPU checks of the stand-alone operators: bad arguments are refused on the host, before anything is launched."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def dare():
+    from paper_2605_08134_b200 import build
+    build.build()
+    from paper_2605_08134_b200 import dare as d
+    return d
+
+
+def _with(cfg, **kw):
+    c = type(cfg).from_buffer_copy(cfg)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+P, Q, R, S = 0x10000, 0x20000, 0x30000, 0x40000        # never dereferenced: every call here is refused (or has nothing to do)
+
+
+def test_rope_table(dare):
+    good = dare.RopeConfig(C.sizeof(dare.RopeConfig), 64, 1e4, 0, 4096, 2.0, 1.0, 32.0, 1.0)
+    assert dare.dare_rope_table(None, P, 8) == dare.ERR_INVALID_ARG
+    assert dare.dare_rope_table(good, None, 8) == dare.ERR_INVALID_ARG
+    inf, nan = float("inf"), float("nan")
+    for kw in (dict(struct_size=8), dict(scaling=5), dict(scaling=-1), dict(theta=0.0), dict(theta=nan), dict(theta=inf),
+               dict(magnitude=nan), dict(scaling=1, factor=0.5), dict(scaling=1, factor=nan), dict(scaling=3, trained=0),
+               dict(scaling=3, low=0.0), dict(scaling=3, low=4.0, high=4.0), dict(scaling=4, high=inf), dict(scaling=4, theta=0.5)):
+        assert dare.dare_rope_table(_with(good, **kw), P, 8) == dare.ERR_INVALID_ARG, kw
+    for kw in (dict(rotary_dim=0), dict(rotary_dim=63), dict(rotary_dim=258), dict(rotary_dim=2, scaling=2)):
+        assert dare.dare_rope_table(_with(good, **kw), P, 8) == dare.ERR_SHAPE, kw
+    assert dare.dare_rope_table(good, P, -1) == dare.ERR_SHAPE
+    assert dare.dare_rope_table(good, P, (1 << 24) + 1) == dare.ERR_SHAPE
+    assert dare.dare_rope_table(good, P + 4, 8) == dare.ERR_ALIGN
+    assert dare.dare_rope_table(good, P, 0) == dare.OK
+
+
+def test_rope(dare):
+    good = dare.RopeApply(C.sizeof(dare.RopeApply), dare.BF16, 4, 2, 64, 64, 0, 0, 0, 128, 64, 128, 64, 100)
+    call = lambda c, x=P, pos=None, t=Q, y=R: dare.dare_rope(c, x, pos, t, y)
+    assert call(None) == dare.ERR_INVALID_ARG
+    for kw in (dict(struct_size=0), dict(dtype=2), dict(layout=2), dict(transpose=2)):
+        assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG, kw
+    for kw in (dict(tokens=-1), dict(tokens=(1 << 30) + 1), dict(heads=-1), dict(head_dim=0), dict(rotary_dim=0), dict(rotary_dim=7),
+               dict(rotary_dim=66), dict(rotary_dim=258, head_dim=512), dict(table_positions=-1), dict(x_token=-1), dict(y_head=63),
+               dict(y_token=63), dict(x_head=-64)):
+        assert call(_with(good, **kw)) == dare.ERR_SHAPE, kw
+    for kw in (dict(x=None), dict(t=None), dict(y=None)):
+        assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
+    assert call(_with(good, x_head=128, x_token=512), y=P) == dare.ERR_INVALID_ARG           # in place with other strides
+    for kw in (dict(x=P + 1), dict(y=R + 1), dict(t=Q + 4), dict(pos=S + 2)):
+        assert call(good, **kw) == dare.ERR_ALIGN, kw
+    assert call(_with(good, tokens=0), x=None) == dare.OK
