@@ -80,6 +80,61 @@ typedef struct {
 dare_status_t dare_rope(const dare_rope_apply_t* cfg, const void* x, const int32_t* positions, const float* table, void* y,
                         int32_t* status, void* cuda_stream);
 
+/* ---- y = act(x W^T + bias) + resid ----------------------------------------------------------------------------------- */
+enum { DARE_ACT_NONE = 0, DARE_ACT_RELU = 1, DARE_ACT_SILU = 2, DARE_ACT_GELU = 3 /* x Phi(x) */, DARE_ACT_GELU_TANH = 4 };
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(dare_linear_config_t) */
+  int32_t dtype;        /* dare_dtype_t of x, W, resid and y; sums in float32 */
+  int64_t rows;         /* <= 2^24; rows * out_features <= 2^38 */
+  int32_t in_features;  /* 1 .. 2^20 */
+  int32_t out_features; /* 1 .. 2^24 */
+  int32_t activation;   /* DARE_ACT_* */
+  int32_t reserved;     /* 0 */
+  int64_t x_row, w_row, resid_row, y_row; /* strides */
+} dare_linear_config_t;
+
+/* x [rows, in_features], w [out_features, in_features] (the layer's convention, y = W x), bias float32 [out_features] or NULL, resid
+ * [rows, out_features] or NULL; resid may be y with the same stride.
+ * bf16 with x, w 16-byte aligned and their strides multiples of 8 runs on the tensor cores, float32 with x, w 16-byte aligned,
+ * strides and in_features multiples of 4 too where that is faster (operands split into three bf16 parts, fp32 accuracy); everything
+ * else on the CUDA cores. */
+dare_status_t dare_linear(const dare_linear_config_t* cfg, const void* x, const void* w, const float* bias, const void* resid,
+                          void* y, int32_t* status, void* cuda_stream);
+
+/* ---- softmax attention over packed sequences --------------------------------------------------------------------------
+ * Sequence b has the query rows [q_begin[b], q_begin[b + 1]) and the key rows k_begin[b] + [0, n_b), n_b = k_len[b], or without k_len
+ * k_begin[b + 1] - k_begin[b].  Query head h reads key/value head h / (n_heads / n_kv_heads).
+ *     out_i = sum_j softmax_j(scale q_i . k_j) v_j    over j < n_b and, if causal, j <= i + n_b - (query rows of b)
+ * (the last query sees every key).  A row that sees no key gets zeros, and -inf as its lse = log sum_j exp(scale q_i . k_j).
+ * Rows of q, out and lse outside every sequence are not touched; k and v are never read into results outside their sequence, and
+ * a key that causality hides from every query of a tile never either; the v rows of a sequence that are hidden from some
+ * queries only must be finite.  One query a sequence is a decoding step; a sequence may be empty. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(dare_attention_config_t) */
+  int32_t dtype;        /* dare_dtype_t of q, k, v and out; softmax in float32 */
+  int32_t batch;        /* sequences, 1 .. 65536 */
+  int32_t n_heads;      /* a multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 32, 64, 128 or 256 */
+  int32_t causal;
+  float scale;          /* > 0 */
+  int64_t q_rows;       /* rows of q, out and lse, <= 2^24 */
+  int64_t k_rows;       /* rows of k and v, < 2^31 */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head; /* strides */
+} dare_attention_config_t;
+
+/* Bytes of device workspace a call needs (16-byte aligned); 0 if the configuration is invalid.  It holds nothing between calls. */
+size_t dare_attention_workspace_bytes(const dare_attention_config_t* cfg);
+
+/* q_begin int32 [batch + 1]; k_begin int32 [batch + 1], or [batch] with k_len int32 [batch]; lse float32 [q_rows, n_heads] or NULL.
+ * A sequence whose slices are not inside q_rows / k_rows is skipped (DARE_ERR_DEVICE_CHECK); query slices must not overlap.
+ * bf16 with head_dim 64 or 128, q, k, v, out 16-byte aligned and strides multiples of 8 runs on the tensor cores, everything else on
+ * the CUDA cores. */
+dare_status_t dare_attention(const dare_attention_config_t* cfg, const void* q, const void* k, const void* v,
+                             const int32_t* q_begin, const int32_t* k_begin, const int32_t* k_len, void* out, float* lse,
+                             void* workspace, size_t workspace_bytes, int32_t* status, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

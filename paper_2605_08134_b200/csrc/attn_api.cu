@@ -1,0 +1,98 @@
+// C entries of the packed attention: argument checks and the choice of a kernel.
+#include <math.h>
+
+#include "attn_packed.h"
+
+using namespace dare;
+
+namespace {
+
+constexpr int kMaxHeads = 1024;
+constexpr int kMinUnits = 2;         // units of kUnitKeys keys that a share has at least
+
+bool valid_config(const dare_attention_config_t* c) {
+  if (!c || c->struct_size != sizeof(dare_attention_config_t)) return false;
+  if (c->dtype != DARE_F32 && c->dtype != DARE_BF16) return false;
+  if (c->causal != 0 && c->causal != 1) return false;
+  if (!(c->scale > 0.f) || !isfinite(c->scale)) return false;
+  return true;
+}
+bool shape_ok(const dare_attention_config_t* c) {
+  if (c->batch <= 0 || c->batch > 65536 || c->n_kv_heads <= 0 || c->n_heads <= 0 || c->n_heads > kMaxHeads ||
+      c->n_heads % c->n_kv_heads != 0)
+    return false;
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return false;
+  if (c->q_rows < 0 || c->q_rows > (int64_t)1 << 24 || c->k_rows < 0 || c->k_rows >= (int64_t)1 << 31) return false;
+  if (c->q_rows * c->n_heads > (int64_t)1 << 31) return false;           // (grids and row numbers stay within 31 bits)
+  const int64_t s[8] = {c->q_token, c->q_head, c->k_token, c->k_head, c->v_token, c->v_head, c->o_token, c->o_head};
+  for (int64_t v : s)
+    if (v < 0 || v >= (int64_t)1 << 38) return false;
+  // (two heads or rows of the output in one place would be written twice)
+  if ((c->n_heads > 1 && c->o_head < c->head_dim) || (c->q_rows > 1 && c->o_token < c->head_dim)) return false;
+  return true;
+}
+bool tc_types(const dare_attention_config_t* c) { return c->dtype == DARE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }
+size_t part_bytes(int rows, int head_dim) { return (size_t)2 * kSms * rows * (head_dim * sizeof(float) + sizeof(float2)); }
+
+}  // namespace
+
+extern "C" {
+
+size_t dare_attention_workspace_bytes(const dare_attention_config_t* c) {
+  if (!valid_config(c) || !shape_ok(c)) return 0;
+  return part_bytes(tc_types(c) ? kTcRows : kSimtRows, c->head_dim);
+}
+
+dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, const void* k, const void* v, const int32_t* q_begin,
+                             const int32_t* k_begin, const int32_t* k_len, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, int32_t* status, void* cuda_stream) {
+  if (!valid_config(c)) return DARE_ERR_INVALID_ARG;
+  if (!shape_ok(c)) return DARE_ERR_SHAPE;
+  if (c->q_rows == 0) return DARE_OK;
+  if (!q || !q_begin || !k_begin || !out || !workspace || (c->k_rows > 0 && (!k || !v))) return DARE_ERR_INVALID_ARG;
+  auto low = [](const void* p, uintptr_t mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; };
+  const uintptr_t elem = c->dtype == DARE_BF16 ? 1u : 3u;
+  if (low(q, elem) || low(k, elem) || low(v, elem) || low(out, elem) || low(q_begin, 3u) || low(k_begin, 3u) || low(k_len, 3u) ||
+      low(lse, 3u) || low(workspace, 15u))
+    return DARE_ERR_ALIGN;
+  if (workspace_bytes < dare_attention_workspace_bytes(c)) return DARE_ERR_WORKSPACE;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+
+  PackedParams p = {};
+  p.q = q; p.k = k; p.v = v; p.o = out; p.lse = lse; p.q_begin = q_begin; p.k_begin = k_begin; p.k_len = k_len; p.status = status;
+  p.q_token = c->q_token; p.q_head = c->q_head; p.k_token = c->k_token; p.k_head = c->k_head;
+  p.v_token = c->v_token; p.v_head = c->v_head; p.o_token = c->o_token; p.o_head = c->o_head;
+  p.q_rows = c->q_rows; p.k_rows = c->k_rows;
+  p.batch = c->batch; p.n_heads = c->n_heads; p.kv_heads = c->n_kv_heads; p.group = c->n_heads / c->n_kv_heads; p.causal = c->causal;
+  p.scale_log2 = c->scale * 1.4426950408889634f;
+  p.n_ctas = kSms;
+  p.min_units = kMinUnits;
+
+  // The tensor-core kernel reads k and v through TMA (16-byte aligned rows and heads with strides of their own), q and out by 16
+  // bytes.
+  auto eights = [](int64_t a) { return a % 8 == 0; };
+  auto tma = [&](int64_t token, int64_t head) {
+    return (c->k_rows <= 1 || (token > 0 && eights(token))) && (c->n_kv_heads <= 1 || (head > 0 && eights(head)));
+  };
+  const bool tc = tc_types(c) && c->k_rows > 0 && !low(q, 15u) && !low(k, 15u) && !low(v, 15u) && !low(out, 15u) && eights(c->q_token) &&
+                  eights(c->q_head) && eights(c->o_token) && eights(c->o_head) && tma(c->k_token, c->k_head) && tma(c->v_token, c->v_head);
+  const int rows = tc ? kTcRows : kSimtRows;
+  p.part_ml = reinterpret_cast<float2*>(workspace);
+  p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * kSms * rows);
+
+  cudaError_t e;
+  if (tc) {
+    // 256 rows a CTA where the sequences have more than one tile's rows on average and that fills the device, shares otherwise.
+    const int64_t all = c->q_rows * p.group;
+    const bool tiles = all > (int64_t)kTcRows * c->batch && (all / 256) * c->n_kv_heads >= 3 * kSms / 4;
+    e = launch_packed_tc(p, c->head_dim, tiles, st);
+    if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);
+  } else {
+    e = launch_packed_simt(p, c->head_dim, c->dtype == DARE_BF16, st);
+    if (e == cudaSuccess) e = launch_packed_combine(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
+  }
+  if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }
+  return DARE_OK;
+}
+
+}  // extern "C"

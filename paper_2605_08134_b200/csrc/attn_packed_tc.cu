@@ -1,0 +1,513 @@
+// Attention over packed sequences on tcgen05 tensor cores: bf16, head_dim 128 or 64, fp32 softmax (attn_packed.h: rows, pairs,
+// tiles and shares).
+//   warps 0, 1   TMA: K and V blocks of 64 keys (64-column boxes, 128-byte swizzle) into rings
+//   warps 2, 3   one lane each issues the products of one stream: S = Q K^T (M 128, N 64) into one of two score buffers, O += P V with
+//                P read from tensor memory
+//   warps 4-11   softmax, four warps a stream, thread <-> row: scores from tensor memory, maximum, 2^x, P as bf16 back over the
+//                scores' columns; O is rescaled in place only when a row's maximum grew by more than 2^8
+// tiles:  a CTA has 256 rows, stream s rows 128 s ..; the streams walk the same blocks and share them: half of what a CTA pulls
+//         from the L2 a flop.  Causal rows see different numbers of blocks; a stream that is through only hands the ring on.
+// shares: a CTA has 128 rows and the streams take its blocks in turn, so that few rows (a decoding step has n_heads / n_kv_heads of
+//         them) still keep 192 KB of keys and values on their way; the streams' results are merged as two parts of a key split.
+//         The producers know a share's segments themselves and run ahead into the next one while the rest of the CTA finishes.
+// P is one bf16 part with heads of 128: its rounding (2^-8 of a weight at most) leaves the output 1.41 times as far from exact as
+// storing it as bf16 does; a second part would be half as much tensor work again.  With heads of 64 it is two (16 bits), as the
+// exponentials and not the products bound those.
+#include "attn_packed.h"
+#include "tc.h"
+#include "tc_ptx.cuh"
+
+namespace dare {
+
+using namespace ptx;
+
+namespace {
+
+constexpr int BQ = kTcRows, BK = 64, kThreads = 384, kSoftmaxThreads = 256, kWorkers = 320;   // workers: all but the producers
+constexpr uint32_t kTmemCols = 512;
+constexpr float kRescaleStep = 8.f;
+template <int HD>
+constexpr bool kSplitP = HD == 64;
+constexpr int one_cta_per_sm(int bytes) { return bytes > 117 * 1024 ? bytes : 117 * 1024; }   // (it takes all tensor memory)
+
+template <int HD, bool TILES>
+struct Smem {
+  static constexpr int Q_BYTES = BQ * HD * 2, KV_BYTES = BK * HD * 2;
+  static constexpr int RING = TILES ? 4 : 6;              // blocks of K and of V; shares: half of them a stream
+  static constexpr int Q_OFF = 0;
+  static constexpr int K_OFF = Q_OFF + (TILES ? 2 : 1) * Q_BYTES;
+  static constexpr int V_OFF = K_OFF + RING * KV_BYTES;
+  static constexpr int BAR_OFF = V_OFF + RING * KV_BYTES;
+  static constexpr int TOTAL = one_cta_per_sm(BAR_OFF + 512 + 1024);
+  static_assert(TOTAL <= 232448, "shared memory of one CTA");
+};
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* tmap, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+// 64 rows (keys) of a head: HD / 64 chunks of 64 columns, counted on one barrier
+template <int HD>
+__device__ __forceinline__ void load_block(uint8_t* dst, const CUtensorMap* tm, bool head_inner, int h, int row, uint64_t* bar) {
+  mbar_arrive_expect_tx(bar, BK * HD * 2);
+#pragma unroll
+  for (int c = 0; c < HD / 64; ++c)
+    tma_load_3d(dst + c * (BK * 128), tm, c * 64, head_inner ? h : row, head_inner ? row : h, bar);
+}
+
+// What a CTA does with one pair, or a part of its keys.
+struct Segment {
+  Place pl;
+  int row0;                      // first row of the CTA's tile in the sequence's rows
+  int rows;                      // its rows (at most 128; tiles: 256)
+  int blk0, n_blk;               // 64-key blocks [blk0, blk0 + n_blk)
+  int slot;                      // < 0: the rows' keys are all here; else the slot of the partial result
+};
+
+// rows and last visible block of 128-row tile `st` of the segment
+__device__ __forceinline__ int stream_rows(const Segment& g, int st) { return max(0, min(BQ, g.rows - st * BQ)); }
+__device__ __forceinline__ int blocks_seen(const PackedParams& p, const Segment& g, int last_row) {
+  return (keys_seen(p, g.pl.s, (g.row0 + last_row) / p.group) + BK - 1) / BK;
+}
+
+// The segment of a share that begins at unit u (shares), or CTA u's pair (tiles); *end: unit behind it.  By a warp.
+template <bool TILES>
+__device__ __forceinline__ bool segment_at(const PackedParams& p, long long u, long long share_begin, long long share_end, Segment* g,
+                                           long long* end) {
+  if (!find_place<TILES ? 2 * BQ : BQ, !TILES>(p, u, &g->pl, nullptr)) return false;
+  constexpr int ROWS = TILES ? 2 * BQ : BQ;
+  g->row0 = g->pl.tile * ROWS;
+  const long long left = (long long)g->pl.s.nq * p.group - g->row0;
+  g->rows = left < ROWS ? (int)left : ROWS;
+  const int seen = blocks_seen(p, *g, g->rows - 1);
+  if (TILES) {
+    g->blk0 = 0;
+    g->n_blk = seen;
+    g->slot = -1;
+    *end = u + 1;
+  } else {
+    const long long pair_end = g->pl.first + g->pl.units;
+    *end = pair_end < share_end ? pair_end : share_end;
+    g->blk0 = (int)(u - g->pl.first) * (kUnitKeys / BK);
+    const int blk1 = min(seen, (int)(*end - g->pl.first) * (kUnitKeys / BK));
+    g->n_blk = max(0, blk1 - g->blk0);
+    const bool whole = u == g->pl.first && *end == pair_end;
+    g->slot = whole ? -1 : 2 * (int)blockIdx.x + (g->pl.first <= share_begin ? 0 : 1);
+  }
+  return true;
+}
+
+}  // namespace
+
+template <int HD, bool TILES>
+__global__ void __launch_bounds__(kThreads, 1)
+packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PackedParams p) {
+  using S = Smem<HD, TILES>;
+  constexpr int RING = TILES ? S::RING : S::RING / 2;         // blocks of a ring (shares: a ring a stream)
+  constexpr int UPR = HD / 8;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);    // [S::RING]
+  uint64_t* k_empty = k_full + S::RING;
+  uint64_t* v_full = k_empty + S::RING;
+  uint64_t* v_empty = v_full + S::RING;
+  uint64_t* s_full = v_empty + S::RING;                        // [2 streams][2 score buffers]
+  uint64_t* p_full = s_full + 4;
+  uint64_t* o_full = p_full + 4;                               // [2 streams][2]: product j signals o_full[stream][j & 1]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 4);
+  __shared__ Segment seg_sh;
+  __shared__ int seg_more;
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::RING; ++i) {
+      mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], TILES ? 2 : 1);
+      mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], TILES ? 2 : 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s_full[i], 1); mbar_init(&o_full[i], 1); mbar_init(&p_full[i], kSoftmaxThreads / 64);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&tm_k);
+    prefetch_tmap(&tm_v);
+  }
+  if (warp == 2) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  // this CTA's part of the launch's line of units (tiles: pair blockIdx.x); warps 0-2 know it
+  long long share_begin = blockIdx.x, share_end = (long long)blockIdx.x + 1;
+  if (!TILES && warp <= 2) {
+    long long total = 0;
+    const long long per = share_units<BQ>(p, &total);
+    share_begin = (long long)blockIdx.x * per;
+    share_end = share_begin + per < total ? share_begin + per : total;
+  }
+
+  const int st = warp < 4 ? (warp & 1) : ((warp - 4) >> 2);                  // stream
+  if (warp < 2) {
+    // ---- producers (tiles: warp 0)
+    if (!TILES || warp == 0) {
+      Segment g;
+      long long u = share_begin, next;
+      uint32_t cnt = 0;
+      for (; u < share_end && segment_at<TILES>(p, u, share_begin, share_end, &g, &next); u = next) {
+        const int n = TILES ? g.n_blk : (g.n_blk - st + 1) / 2;
+        for (int j = 0; j < n; ++j, ++cnt) {
+          const int slot = (TILES ? 0 : st * RING) + (int)(cnt % RING);
+          const uint32_t freed = ((cnt / RING) & 1) ^ 1;
+          const int row = g.pl.s.k0 + (g.blk0 + (TILES ? j : 2 * j + st)) * BK;
+          mbar_wait(&k_empty[slot], freed, p.status);
+          if (elect_one()) load_block<HD>(smem + S::K_OFF + slot * S::KV_BYTES, &tm_k, p.k_head_inner, g.pl.h, row, &k_full[slot]);
+          __syncwarp();
+          mbar_wait(&v_empty[slot], freed, p.status);
+          if (elect_one()) load_block<HD>(smem + S::V_OFF + slot * S::KV_BYTES, &tm_v, p.v_head_inner, g.pl.h, row, &v_full[slot]);
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    const uint32_t tmem_s = tmem_base + st * 2 * BK, tmem_o = tmem_base + 4 * BK + st * HD;
+    long long u = share_begin, next = 0;
+    uint32_t cnt = 0;                        // blocks of this stream so far: score buffer cnt & 1
+    uint32_t kcnt = 0;                       // ring position (tiles: blocks of both streams)
+    for (;;) {
+      // everybody is through with the segment before: its Q tile, its accumulators
+      asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
+      if (warp == 2) {
+        Segment g;
+        const bool more = u < share_end && segment_at<TILES>(p, u, share_begin, share_end, &g, &next);
+        u = next;
+        if (lane == 0) {
+          seg_more = more ? 1 : 0;
+          if (more) seg_sh = g;
+        }
+      }
+      asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
+      if (!seg_more) break;
+      const Segment g = seg_sh;
+      // ---- Q rows -> shared memory, K-major, 128-byte swizzle
+      {
+        constexpr int TILE_UNITS = BQ * UPR, QU = ((TILES ? 2 : 1) * TILE_UNITS + kWorkers - 1) / kWorkers;
+        const int units = ((g.rows + BQ - 1) / BQ) * TILE_UNITS, u0 = (int)threadIdx.x - 64;
+        const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q);
+        uint4 qv[QU];
+#pragma unroll
+        for (int i = 0; i < QU; ++i) {
+          const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR;
+          qv[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (w < units && r < g.rows) {
+            const RowAt at = row_at(p, g.pl, g.row0 + r);
+            qv[i] = __ldcg(reinterpret_cast<const uint4*>(q + (long long)(g.pl.s.q0 + at.query) * p.q_token + at.head * p.q_head + unit * 8));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < QU; ++i) {
+          const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR, rt = r & (BQ - 1);
+          if (w < units)
+            *reinterpret_cast<uint4*>(smem + S::Q_OFF + (r / BQ) * S::Q_BYTES + (unit >> 3) * (BQ * 128) + rt * 128 +
+                                      (((unit & 7) ^ (rt & 7)) << 4)) = qv[i];
+        }
+        fence_proxy_async_smem();
+      }
+      asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
+
+      const int rows = TILES ? stream_rows(g, st) : g.rows;            // of this stream
+      const int tile_row = g.row0 + (TILES ? st * BQ : 0);
+      // blocks of this stream; tiles: of the g.n_blk that pass through the ring
+      const int n_st = TILES ? (rows > 0 ? min(g.n_blk, blocks_seen(p, g, st * BQ + rows - 1)) : 0) : (g.n_blk - st + 1) / 2;
+      if (warp < 4) {
+        // ---- issuer of this stream's products
+        constexpr uint32_t idesc_qk = idesc_bf16(BQ, BK, false), idesc_pv = idesc_bf16(BQ, HD, true);
+        const uint64_t q_desc = smem_desc_k_sw128(smem_u32(smem + S::Q_OFF + (TILES ? st * S::Q_BYTES : 0)));
+        const uint64_t k_desc0 = smem_desc_k_sw128(smem_u32(smem + S::K_OFF));
+        const uint64_t v_desc0 = smem_desc_mn_sw128(smem_u32(smem + S::V_OFF), BK * 128);
+        const int ring0 = TILES ? 0 : st * RING;
+        auto issue_qk = [&](int j) {
+          const uint32_t kc = kcnt + j, sb = (cnt + j) & 1;
+          const int slot = ring0 + (int)(kc % RING);
+          mbar_wait(&k_full[slot], (kc / RING) & 1, p.status);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t k_desc = k_desc0 + (uint64_t)(slot * (S::KV_BYTES >> 4));
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk)
+              umma_ss(tmem_s + sb * BK, q_desc + (((kk >> 2) * (BQ * 128) + (kk & 3) * 32) >> 4),
+                      k_desc + (((kk >> 2) * (BK * 128) + (kk & 3) * 32) >> 4), idesc_qk, kk != 0 ? 1u : 0u);
+            umma_commit(&s_full[2 * st + sb]);
+            umma_commit(&k_empty[slot]);
+          }
+          __syncwarp();
+        };
+        if (n_st > 0) issue_qk(0);
+        if (n_st > 1) issue_qk(1);
+        for (int j = 0; j < n_st; ++j) {
+          const uint32_t kc = kcnt + j, sc = cnt + j, sb = sc & 1;
+          const int slot = ring0 + (int)(kc % RING);
+          mbar_wait(&p_full[2 * st + sb], (sc >> 1) & 1, p.status);          // P(j) has replaced S(j)
+          mbar_wait(&v_full[slot], (kc / RING) & 1, p.status);
+          // rows behind the sequence's last key are whatever lies there, and 0 * inf would be NaN: they become zeros
+          const int keys = g.pl.s.n - (g.blk0 + (TILES ? j : 2 * j + st)) * BK;
+          if (keys < BK) {
+            uint8_t* v = smem + S::V_OFF + slot * S::KV_BYTES;
+            for (int i = lane; i < (BK - keys) * UPR; i += 32) {
+              const int r = keys + i / UPR, unit = i % UPR;
+              *reinterpret_cast<uint4*>(v + (unit >> 3) * (BK * 128) + r * 128 + ((unit & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t v_desc = v_desc0 + (uint64_t)(slot * (S::KV_BYTES >> 4));
+#pragma unroll
+            for (int ks = 0; ks < BK / 16; ++ks) {
+              umma_ts(tmem_o, tmem_s + sb * BK + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, (j | ks) != 0 ? 1u : 0u);
+              if (kSplitP<HD>) umma_ts(tmem_o, tmem_s + sb * BK + 32 + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, 1u);
+            }
+            umma_commit(&o_full[2 * st + sb]);
+            umma_commit(&v_empty[slot]);
+          }
+          __syncwarp();
+          if (j + 2 < n_st) issue_qk(j + 2);          // (in issue order behind the product that reads P(j))
+        }
+        if (TILES) {
+          for (int j = n_st; j < g.n_blk; ++j) {      // blocks that only the other stream's rows see
+            const uint32_t kc = kcnt + j;
+            const int slot = (int)(kc % RING);
+            mbar_wait(&k_full[slot], (kc / RING) & 1, p.status);
+            if (elect_one()) mbar_arrive(&k_empty[slot]);
+            __syncwarp();
+            mbar_wait(&v_full[slot], (kc / RING) & 1, p.status);
+            if (elect_one()) mbar_arrive(&v_empty[slot]);
+            __syncwarp();
+          }
+        }
+      } else {
+        // ---- softmax of this stream's rows
+        const int quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+        const float c = p.scale_log2;
+        const bool warp_has_rows = quarter * 32 < rows;
+        const RowAt at = row_at(p, g.pl, tile_row + min(r, max(rows - 1, 0)));
+        const int seen = keys_seen(p, g.pl.s, at.query);
+        float m = -INFINITY, l = 0.f;               // maximum the exponentials are taken against; sum against it
+        for (int j = 0; j < n_st; ++j) {
+          const uint32_t sc = cnt + j, sb = sc & 1, sbuf = tmem_s + sb * BK + lane_addr;
+          mbar_wait(&s_full[2 * st + sb], (sc >> 1) & 1, p.status);
+          tc_fence_after();
+          if (!warp_has_rows) {                     // rows of no query: only hand the block on
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[2 * st + sb]);
+            continue;
+          }
+          const int keys = seen - (g.blk0 + (TILES ? j : 2 * j + st)) * BK;     // of the block that this row sees
+          float v[BK];
+          tmem_ld_32x32_nowait(sbuf, v);
+          tmem_ld_32x32_nowait(sbuf + 32, v + 32);
+          tmem_ld_wait();
+          if (__any_sync(0xffffffffu, keys < BK)) {
+#pragma unroll
+            for (int i = 0; i < BK; ++i)
+              if (i >= keys) v[i] = -INFINITY;
+          }
+          float mx4[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx4[k] = fmaxf(v[k], v[4 + k]);
+#pragma unroll
+          for (int i = 8; i < BK; i += 8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx4[k] = fmax3(mx4[k], v[i + k], v[i + 4 + k]);
+          }
+          const float m_new = fmax3(m, fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+          if (j == 0) {
+            m = m_new;
+          } else {
+            const bool grow = (m_new - m) * c > kRescaleStep;        // (-inf to -inf: NaN, no)
+            if (__any_sync(0xffffffffu, grow)) {
+              const float alpha = grow ? fast_exp2((m - m_new) * c) : 1.f;
+              if (grow) { m = m_new; l *= alpha; }
+              mbar_wait(&o_full[2 * st + (sb ^ 1)], ((sc - 1) >> 1) & 1, p.status);     // product j - 1 has been added
+              tc_fence_after();
+#pragma unroll 1
+              for (int ch = 0; ch < HD / 32; ++ch) {
+                float o[32];
+                tmem_ld_32x32(tmem_o + lane_addr + ch * 32, o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= alpha;
+                tmem_st_32x32(tmem_o + lane_addr + ch * 32, o);
+              }
+            }
+          }
+          const float mc = m == -INFINITY ? 0.f : m * c;             // (nothing seen yet: 2^-inf = 0, not 2^NaN)
+          const float2 c2 = make_float2(c, c), nmc2 = make_float2(-mc, -mc);
+          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          float pk[BK / 2], pl[kSplitP<HD> ? BK / 2 : 1];
+#pragma unroll
+          for (int i = 0; i < BK; i += 2) {
+            float2 e = __ffma2_rn(make_float2(v[i], v[i + 1]), c2, nmc2);
+            e.x = fast_exp2(e.x);
+            e.y = fast_exp2(e.y);
+            sum2[(i >> 1) & 1] = __fadd2_rn(sum2[(i >> 1) & 1], e);
+            __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
+            pk[i >> 1] = __uint_as_float(*reinterpret_cast<uint32_t*>(&h2));
+            if (kSplitP<HD>) {
+              const float2 rest = __fadd2_rn(e, make_float2(-__low2float(h2), -__high2float(h2)));
+              __nv_bfloat162 l2 = __floats2bfloat162_rn(rest.x, rest.y);
+              pl[kSplitP<HD> ? i >> 1 : 0] = __uint_as_float(*reinterpret_cast<uint32_t*>(&l2));
+            }
+          }
+          tmem_st_32x32_nowait(sbuf, pk);
+          if (kSplitP<HD>) tmem_st_32x32_nowait(sbuf + 32, pl);
+          tmem_st_wait();
+          l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full[2 * st + sb]);
+        }
+        for (int j = max(0, n_st - 2); j < n_st; ++j)                // the last two products
+          mbar_wait(&o_full[2 * st + ((cnt + j) & 1)], ((cnt + j) >> 1) & 1, p.status);
+        tc_fence_after();
+
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o) + (long long)(g.pl.s.q0 + at.query) * p.o_token + at.head * p.o_head;
+        float* lse = p.lse ? p.lse + (long long)(g.pl.s.q0 + at.query) * p.n_heads + at.head : nullptr;
+        if (TILES) {
+          if (warp_has_rows) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+            for (int ch = 0; ch < HD / 32; ++ch) {
+              float o[32];
+              if (n_st > 0) {
+                tmem_ld_32x32(tmem_o + lane_addr + ch * 32, o);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0.f;
+              }
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] *= inv;
+              if (r < rows) {
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) reinterpret_cast<uint4*>(dst + ch * 32)[q4] = pack8_bf16(o + 8 * q4);
+              }
+            }
+            if (lse && r < rows) *lse = l == 0.f ? -INFINITY : (m * c) * 0.69314718055994531f + logf(l);
+          }
+        } else {
+          // ---- merge the two streams: thread (stream, row) finishes its half of the row's columns.  The statistics go where the Q
+          // tile was: both streams' last products are complete behind the first barrier.
+          constexpr int HC = HD / 2;
+          float2* stat = reinterpret_cast<float2*>(smem + S::Q_OFF);
+          asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+          stat[st * BQ + r] = make_float2(m, l);
+          tc_fence_before();
+          asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+          tc_fence_after();
+          if (warp_has_rows) {
+            const int n_other = g.n_blk - n_st;
+            const float2 other = stat[(st ^ 1) * BQ + r];
+            const float m_all = fmaxf(m, other.x);
+            const float w_mine = m == -INFINITY ? 0.f : fast_exp2((m - m_all) * c);
+            const float w_other = other.x == -INFINITY ? 0.f : fast_exp2((other.x - m_all) * c);
+            const float l_row = w_mine * l + w_other * other.y;
+            const float inv = g.slot >= 0 ? 1.f : (l_row == 0.f ? 0.f : 1.f / l_row);
+            const uint32_t t_mine = tmem_o + lane_addr + st * HC;
+            const uint32_t t_other = tmem_base + 4 * BK + (st ^ 1) * HD + lane_addr + st * HC;
+            float* part = p.part_o + ((size_t)max(g.slot, 0) * BQ + r) * HD + st * HC;
+#pragma unroll 1
+            for (int ch = 0; ch < HC / 32; ++ch) {
+              float o[32], a[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = 0.f;
+              if (n_st > 0) {
+                tmem_ld_32x32(t_mine + ch * 32, a);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = a[i] * w_mine;
+              }
+              if (n_other > 0) {
+                tmem_ld_32x32(t_other + ch * 32, a);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = fmaf(a[i], w_other, o[i]);
+              }
+              if (r < rows) {
+                if (g.slot >= 0) {
+#pragma unroll
+                  for (int q4 = 0; q4 < 8; ++q4)
+                    reinterpret_cast<float4*>(part + ch * 32)[q4] = make_float4(o[4 * q4], o[4 * q4 + 1], o[4 * q4 + 2], o[4 * q4 + 3]);
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) o[i] *= inv;
+#pragma unroll
+                  for (int q4 = 0; q4 < 4; ++q4) reinterpret_cast<uint4*>(dst + st * HC + ch * 32)[q4] = pack8_bf16(o + 8 * q4);
+                }
+              }
+            }
+            if (st == 0 && r < rows) {
+              if (g.slot >= 0) p.part_ml[(size_t)g.slot * BQ + r] = make_float2(m_all * c, l_row);
+              else if (lse) *lse = l_row == 0.f ? -INFINITY : (m_all * c) * 0.69314718055994531f + logf(l_row);
+            }
+          }
+          tc_fence_before();
+        }
+      }
+      cnt += n_st;
+      kcnt += TILES ? g.n_blk : n_st;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+namespace {
+// [rows][heads][head_dim] with any strides as a tensor map of boxes 64 columns x 64 rows of one head; the dimension with the smaller
+// stride comes first.  A dimension of one entry has no stride of its own.
+bool make_head_map(CUtensorMap* m, const void* base, int head_dim, uint64_t heads, uint64_t rows, long long head_stride, long long row_stride,
+                   int* head_inner) {
+  if (heads == 1) head_stride = head_dim;
+  if (rows == 1) row_stride = head_stride * (long long)heads;
+  *head_inner = head_stride <= row_stride ? 1 : 0;
+  return make_map_3d(m, base, head_dim, *head_inner ? heads : rows, *head_inner ? rows : heads, *head_inner ? head_stride : row_stride,
+                     *head_inner ? row_stride : head_stride, *head_inner ? 1 : BK, *head_inner ? BK : 1);
+}
+
+template <int HD, bool TILES>
+cudaError_t launch_as(PackedParams p, cudaStream_t st) {
+  static std::atomic<unsigned long long> attr{0};
+  auto kern = packed_tc_kernel<HD, TILES>;
+  if (cudaError_t e = ensure_dyn_smem(kern, Smem<HD, TILES>::TOTAL, attr); e != cudaSuccess) return e;
+  CUtensorMap mk, mv;
+  if (!make_head_map(&mk, p.k, HD, p.kv_heads, p.k_rows, p.k_head, p.k_token, &p.k_head_inner) ||
+      !make_head_map(&mv, p.v, HD, p.kv_heads, p.k_rows, p.v_head, p.v_token, &p.v_head_inner))
+    return cudaErrorInvalidValue;
+  // tiles: as many CTAs as there can be pairs (a sequence's last tile may be partly filled); those behind the last one leave
+  const long long grid = TILES ? ((p.q_rows * p.group) / (2 * BQ) + p.batch) * p.kv_heads : p.n_ctas;
+  return launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), Smem<HD, TILES>::TOTAL, st, 1, mk, mv, p);
+}
+}  // namespace
+
+cudaError_t launch_packed_tc(const PackedParams& p, int head_dim, bool tiles, cudaStream_t st) {
+  if (head_dim == 128) return tiles ? launch_as<128, true>(p, st) : launch_as<128, false>(p, st);
+  return tiles ? launch_as<64, true>(p, st) : launch_as<64, false>(p, st);
+}
+
+}  // namespace dare

@@ -30,6 +30,9 @@
 //   warps 4-11  fetch the operands (16 bytes a lane, whole lines), a block ahead of the one they split, and write the parts
 //               into a ring of two stages (72 KB each: 192 rows x 64 k x 3 parts) in the 128-byte-swizzled layout
 //   warp 12     issues the 16 MMAs (M 128, N 64 or 128, K 16) of a block
+#include <type_traits>
+
+#include "linear.h"
 #include "sgemm.h"
 #include "tc_ptx.cuh"
 
@@ -74,8 +77,16 @@ __device__ __forceinline__ float4 load_now(const float* p) {
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 }  // namespace
 
+// What a launch takes: a projection's parameters (SG_Q, SG_KV, SG_OUT), or those of the stand-alone product (SG_LINEAR): any
+// number of outputs and of k-elements (multiples of 4), strides, and its own tail; rows and columns past the end are read as the
+// last one, k-elements past the end as zeros.
+constexpr int SG_LINEAR = 3;
 template <int EPI>
-__global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const SgemmParams p) {
+using Params = typename std::conditional<EPI == SG_LINEAR, LinearParams, SgemmParams>::type;
+
+template <int EPI>
+__global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI> p) {
+  constexpr bool LINEAR = EPI == SG_LINEAR;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + BAR_OFFSET);
@@ -90,17 +101,29 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const SgemmParams
   __shared__ int s_tok[BM], s_pos[BM];
   __shared__ size_t s_row[BM], s_crow[BM];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = (int)threadIdx.x;
-  const int K = p.g.d, half = p.g.head_dim >> 1, lh = 31 - __clz(half), KB = K / BK;
-  const int n_tiles = K / BN;
+  int K, half = 32, lh = 5, n_tiles = 1 << 30;
+  if constexpr (LINEAR) {
+    K = p.k;
+  } else {
+    K = p.g.d; half = p.g.head_dim >> 1; lh = 31 - __clz(half);
+    n_tiles = K / BN;
+  }
+  const int KB = LINEAR ? (K + BK - 1) / BK : K / BK;
   const bool second = EPI == SG_KV && (int)blockIdx.x >= n_tiles;
   const int pair0 = ((int)blockIdx.x - (second ? n_tiles : 0)) * (BN / 2);
-  const float* w = reinterpret_cast<const float*>(second ? p.w1 : p.w0);
+  const float* w;
+  if constexpr (LINEAR) w = reinterpret_cast<const float*>(p.w);
+  else w = reinterpret_cast<const float*>(second ? p.w1 : p.w0);
   auto column = [&](int pair) { return (pair >> lh) * (2 * half) + (pair & (half - 1)); };
   const int m0 = (int)(blockIdx.z * gridDim.y + blockIdx.y) * BM;
-  // (row tiles past the first of a gathered launch are usually empty: they look at the count first)
-  if (p.count != nullptr && m0 > 0) {
-    pdl_wait();
-    if (m0 >= checked_count(*p.count, p.rows, p.status)) return;
+  if constexpr (LINEAR) {
+    if (m0 >= p.rows) return;                    // (the grid's last rows)
+  } else {
+    // (row tiles past the first of a gathered launch are usually empty: they look at the count first)
+    if (p.count != nullptr && m0 > 0) {
+      pdl_wait();
+      if (m0 >= checked_count(*p.count, p.rows, p.status)) return;
+    }
   }
   if (tid == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], kSplitters / 32); mbar_init(&empty_bar[s], 1); }
@@ -121,15 +144,20 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const SgemmParams
 #pragma unroll
     for (int i = 0; i < W_CHUNKS; ++i) {
       const int row = row_of + ROWS * i;
-      src[i] = w + (size_t)(column(pair0 + (row & 31)) + (row >> 5) * half) * K + kc;
-      v0[i] = load_now(src[i]);
+      if constexpr (LINEAR) {
+        src[i] = w + (long long)min(2 * pair0 + row, p.n - 1) * p.w_row + kc;
+      } else {
+        src[i] = w + (size_t)(column(pair0 + (row & 31)) + (row >> 5) * half) * K + kc;
+        v0[i] = load_now(src[i]);
+      }
     }
   }
   pdl_wait();
   pdl_launch_dependents();
-  const int m_eff = p.count ? checked_count(*p.count, p.rows, p.status) : p.rows;
+  int m_eff = p.rows;
+  if constexpr (!LINEAR) m_eff = p.count ? checked_count(*p.count, p.rows, p.status) : p.rows;
   const bool active = m0 < m_eff;                // uniform over the CTA
-  if (tid < BM) {
+  if constexpr (!LINEAR) if (tid < BM) {
     int t = m0 + tid < m_eff ? (p.idx ? p.idx[m0 + tid] : m0 + tid) : -1;
     if (p.idx && t != -1 && !token_ok(t, p.g.tokens(), p.status)) t = -1;   // (not written)
     const int tc = max(t, 0);
@@ -145,22 +173,31 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const SgemmParams
   if (active && splitter) {
 #pragma unroll
     for (int i = W_CHUNKS; i < CHUNKS; ++i) {
-      src[i] = reinterpret_cast<const float*>(p.a) + s_row[row_of + ROWS * i - BN] * K + kc;
-      v0[i] = load_now(src[i]);
+      if constexpr (LINEAR) src[i] = reinterpret_cast<const float*>(p.x) + (long long)min(m0 + row_of + ROWS * i - BN, p.rows - 1) * p.x_row + kc;
+      else src[i] = reinterpret_cast<const float*>(p.a) + s_row[row_of + ROWS * i - BN] * K + kc;
+      if constexpr (!LINEAR) v0[i] = load_now(src[i]);
     }
+    if constexpr (LINEAR) {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) v0[i] = kc < K ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    int k_at = 0;                                // (SG_LINEAR: k-element src stands at, less kc)
     // Even blocks come into registers, odd ones into a slot of shared memory (a thread's own chunks: nobody else waits for
     // them), the next on its way while one is split.
     auto fetch = [&]() {
+      const bool there = !LINEAR || k_at + kc < K;
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) v0[i] = load_now(src[i]);
+      for (int i = 0; i < CHUNKS; ++i) v0[i] = there ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
     };
     float* slot = reinterpret_cast<float*>(smem + SLOT_OFFSET) + st_id * 4;
     auto fetch_slot = [&]() {
+      const bool there = !LINEAR || k_at + BK + kc < K;      // (else zeros; the address is valid all the same)
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
-        cp_async_16(smem_u32(slot + i * (kSplitters * 4)), src[i] + BK, 16u);
+        cp_async_16(smem_u32(slot + i * (kSplitters * 4)), there ? src[i] + BK : src[i] - (LINEAR ? k_at + kc : 0), there ? 16u : 0u);
         src[i] += 2 * BK;                        // (the next even block)
       }
+      if (LINEAR) k_at += 2 * BK;
       cp_async_commit();
     };
     auto split2 = [](float x, float y, uint32_t (&o)[3]) {
@@ -303,7 +340,35 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const SgemmParams
     for (int c = 0; c < BN; c += 4)
       *reinterpret_cast<float4*>(tile + tid * TILE_PITCH + c) = make_float4(acc[c / 2].x, acc[c / 2].y, acc[c / 2 + 1].x, acc[c / 2 + 1].y);
   }
-  if (active) {
+  if constexpr (LINEAR) {
+    // ---- bias, activation, residual: a warp a row, two columns a lane
+    const float* bias = p.bias;
+    const int n0 = 2 * pair0, c[2] = {n0 + lane, n0 + 32 + lane};
+    float bv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) bv[i] = bias && c[i] < p.n ? bias[c[i]] : 0.f;
+    __syncthreads();
+    for (int r = warp; r < BM && m0 + r < p.rows; r += kThreads / 32) {
+      const long long row = m0 + r;
+      float v[2] = {tile[r * TILE_PITCH + lane], tile[r * TILE_PITCH + 32 + lane]};
+      if (!finite(v[0]) || !finite(v[1])) {
+        const int last = p.n - 1;
+        const float2 ab = plain_dots(reinterpret_cast<const float*>(p.x) + row * p.x_row, w + (long long)min(c[0], last) * p.w_row,
+                                     w + (long long)min(c[1], last) * p.w_row, K);
+        if (!finite(v[0])) v[0] = ab.x;
+        if (!finite(v[1])) v[1] = ab.y;
+      }
+      v[0] += bv[0];
+      v[1] += bv[1];
+      activate(v, p.act);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (c[i] < p.n) {
+          if (p.resid) v[i] += reinterpret_cast<const float*>(p.resid)[row * p.resid_row + c[i]];
+          reinterpret_cast<float*>(p.y)[row * p.y_row + c[i]] = v[i];
+        }
+    }
+  } else if (active) {
     // ---- the projection's own tail: a warp a row, lane <-> rotary pair, the table reads of four rows in flight together
     constexpr int NW = kThreads / 32, RB = 5;    // rows warp, warp + 13, ...: two batches of five
     const bool rotate = EPI == SG_Q || (EPI == SG_KV && !second);
@@ -384,6 +449,13 @@ static cudaError_t launch_as(const SgemmParams& p, cudaStream_t st) {
   const int row_tiles = (p.rows + BM - 1) / BM, nz = (row_tiles + 65534) / 65535;
   return launch_pdl(gemm_f32_kernel<EPI>, dim3(p.g.d / BN * (EPI == SG_KV ? 2 : 1), (row_tiles + nz - 1) / nz, nz), dim3(kThreads),
                     SMEM_TOTAL, st, 1, p);
+}
+cudaError_t launch_linear_f32(const LinearParams& p, cudaStream_t st) {
+  static std::atomic<unsigned long long> attr_done{0};
+  if (cudaError_t e = ensure_dyn_smem(gemm_f32_kernel<SG_LINEAR>, SMEM_TOTAL, attr_done); e != cudaSuccess) return e;
+  const int row_tiles = (p.rows + BM - 1) / BM, nz = (row_tiles + 65534) / 65535;
+  return launch_pdl(gemm_f32_kernel<SG_LINEAR>, dim3((p.n + BN - 1) / BN, (row_tiles + nz - 1) / nz, nz), dim3(kThreads), SMEM_TOTAL, st, 1,
+                    p);
 }
 cudaError_t launch_gemm_f32(int epi, const SgemmParams& p, cudaStream_t st) {
   if (p.rows <= 0) return cudaSuccess;

@@ -1,0 +1,53 @@
+// y = act(x W^T + bias) + resid (dare_ops.h): what its kernels share.
+#pragma once
+
+#include "ops.h"
+
+namespace dare {
+
+struct LinearParams {
+  const void* x;
+  const void* w;
+  const float* bias;         // or nullptr
+  const void* resid;         // or nullptr
+  void* y;
+  long long x_row, w_row, resid_row, y_row;
+  int rows, n, k, act;
+  int* status;
+};
+
+#ifdef __CUDACC__
+// v[i] = act(v[i]); one switch for all of them
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act) {
+  switch (act) {
+    case DARE_ACT_RELU:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                                     // (NaN stays)
+      break;
+    case DARE_ACT_SILU:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = v[i] / (1.f + expf(-v[i]));
+      break;
+    case DARE_ACT_GELU:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+      break;
+    case DARE_ACT_GELU_TANH:
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        v[i] = 0.5f * v[i] * (1.f + tanhf(0.79788456080286536f * (v[i] + 0.044715f * v[i] * v[i] * v[i])));
+      break;
+    default: break;
+  }
+}
+#endif
+
+// bf16 on the tensor cores (linear_tc.cu): x, w 16-byte aligned, strides multiples of 8
+cudaError_t launch_linear_tc(const LinearParams& p, cudaStream_t st);
+// float32 on the tensor cores, operands in three bf16 parts (gemm_f32.cu): x, w 16-byte aligned, k and strides multiples of 4
+cudaError_t launch_linear_f32(const LinearParams& p, cudaStream_t st);
+// either type on the CUDA cores, any alignment (linear.cu)
+cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, cudaStream_t st);
+
+}  // namespace dare

@@ -1,0 +1,285 @@
+// y = act(x W^T + bias) + resid in bf16 on tcgen05 tensor cores, any number of rows and outputs (dare_ops.h).
+// Persistent: a CTA (or a pair of CTAs sharing M = 256 MMAs, cta_group::2) walks output tiles of 128 (256) rows x `width` columns, the
+// finishing pass of a tile running beside the next one's main loop.  The width is not fixed: it is what the launch rule below
+// finds cheapest, a multiple of 16 up to 256.  With few rows the launch is a stream of W and the width is the outputs over the SMs,
+// so that every SM pulls its share at the same time and no reduction has to be split; only the rows there are come into shared
+// memory then (the MMA's other rows read whatever follows, and nobody reads their results), which leaves up to 24 stages of W on
+// their way.
+//   warp 0     TMA producer: rows of x and of W, 64 k-elements a stage; rows, columns and k-elements past the end are zeros
+//   warp 1     MMA issuer (of a pair: the even CTA's), two accumulators of up to 256 columns of tensor memory in turn
+//   warps 2-9  finishing pass, two warps a lane quarter, thread <-> row, 32 columns at a time: bias, activation, residual, store
+#include "linear.h"
+#include "tc.h"
+#include "tc_ptx.cuh"
+
+namespace dare {
+
+using namespace ptx;
+
+namespace {
+constexpr int BM = 128, BK = 64, kFinish = 8, kThreads = (2 + kFinish) * 32;
+constexpr int kRing = 192 * 1024, kMaxStages = 24;
+constexpr int BAR_OFFSET = kRing + BM * BK * 2;            // (an MMA reads 128 rows from where a stage's rows of x begin)
+constexpr int SMEM_TOTAL = BAR_OFFSET + 512 + 1024;
+static_assert(SMEM_TOTAL <= 227 * 1024 && (2 * kMaxStages + 4) * 8 + 4 <= 512, "shared memory of one CTA");
+constexpr int kGroupBytes = 24 << 20;                      // column tiles are walked in groups of this much of W, as in gemm_persist.cu
+
+struct TileWalk {
+  int width, x_rows;          // columns of a tile; rows of x a stage holds
+  int n_tiles, m_units;       // column tiles; row tiles (PAIR: pairs of them)
+  int n_group;
+  int wide_y, wide_bias;      // y (and resid) by 16 bytes, bias by 16 bytes
+};
+
+template <bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const LinearParams p,
+                 const TileWalk t) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + BAR_OFFSET);
+  uint64_t* empty_bar = full_bar + kMaxStages;
+  uint64_t* acc_full = empty_bar + kMaxStages;       // [2]
+  uint64_t* acc_empty = acc_full + 2;                // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int pr = PAIR ? (int)cluster_ctarank() : 0;
+  const int walker = PAIR ? (int)blockIdx.x / 2 : (int)blockIdx.x, n_walkers = PAIR ? (int)gridDim.x / 2 : (int)gridDim.x;
+  const int w_rows = PAIR ? t.width / 2 : t.width, x_bytes = t.x_rows * BK * 2, stage_bytes = x_bytes + w_rows * BK * 2;
+  const int stages = min(kMaxStages, kRing / stage_bytes), KB = (p.k + BK - 1) / BK, total = t.n_tiles * t.m_units;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], PAIR ? 2 * kFinish : kFinish); }
+    fence_mbar_init();
+    prefetch_tmap(&tm_x);
+    prefetch_tmap(&tm_w);
+  }
+  if (warp == 1) {
+    if (PAIR) { tmem_alloc2(tmem_slot, 512); tmem_relinquish2(); }
+    else { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+  }
+  tc_fence_before();
+  __syncthreads();
+  uint32_t tmem_base;
+  if (PAIR) {
+    cluster_sync_all();              // both CTAs have their barriers and tensor memory before either touches the other's
+    tc_fence_after();
+    tmem_base = ld_cluster_u32(map_to_cta(smem_u32(tmem_slot), 0));
+  } else {
+    tc_fence_after();
+    tmem_base = *tmem_slot;
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+
+  auto tile_of = [&](int u, int* m0, int* n0) {
+    int width = t.n_tiles, nt0 = 0, r = u;
+    if (t.n_group < t.n_tiles) {
+      const int in_group = t.n_group * t.m_units, grp = u / in_group;
+      r = u - grp * in_group;
+      nt0 = grp * t.n_group;
+      width = min(t.n_group, t.n_tiles - nt0);
+    }
+    const int mu = r / width;
+    *m0 = (PAIR ? 2 * mu + pr : mu) * BM;
+    *n0 = (nt0 + r - mu * width) * t.width;
+  };
+  if (warp == 0) {
+    uint32_t it = 0;
+    for (int u = walker; u < total; u += n_walkers) {
+      int m0, n0;
+      tile_of(u, &m0, &n0);
+      for (int kb = 0; kb < KB; ++kb, ++it) {
+        const int s = it % stages;
+        mbar_wait(&empty_bar[s], ((it / stages) & 1) ^ 1, p.status);
+        if (elect_one()) {
+          uint8_t* dst = smem + s * stage_bytes;
+          if (PAIR) {                 // the bytes of both CTAs are counted on the even one's barrier
+            const uint32_t fb = map_to_cta(smem_u32(&full_bar[s]), 0);
+            if (pr == 0) mbar_arrive_expect_tx(&full_bar[s], 2u * stage_bytes);
+            tma_load_2d_pair(dst, &tm_x, kb * BK, m0, fb);
+            tma_load_2d_pair(dst + x_bytes, &tm_w, kb * BK, n0 + pr * w_rows, fb);
+          } else {
+            mbar_arrive_expect_tx(&full_bar[s], (uint32_t)stage_bytes);
+            tma_load_2d(dst, &tm_x, kb * BK, m0, &full_bar[s]);
+            tma_load_2d(dst + x_bytes, &tm_w, kb * BK, n0, &full_bar[s]);
+          }
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 1) {
+    if (pr == 0) {
+      const uint32_t idesc = idesc_bf16(PAIR ? 2 * BM : BM, t.width);
+      uint32_t it = 0, tcount = 0;
+      for (int u = walker; u < total; u += n_walkers, ++tcount) {
+        const uint32_t buf = tcount & 1, d_tmem = tmem_base + buf * 256;
+        mbar_wait(&acc_empty[buf], ((tcount >> 1) & 1) ^ 1, p.status);
+        tc_fence_after();
+        for (int kb = 0; kb < KB; ++kb, ++it) {
+          const int s = it % stages;
+          mbar_wait(&full_bar[s], (it / stages) & 1, p.status);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t at = smem_u32(smem + s * stage_bytes);
+            const uint64_t a = smem_desc_k_sw128(at), b = smem_desc_k_sw128(at + x_bytes);
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k) {
+              if (PAIR) umma2_ss(d_tmem, a + 2 * k, b + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
+              else umma_ss(d_tmem, a + 2 * k, b + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
+            }
+            if (PAIR) {
+              umma2_commit(map_to_cta(smem_u32(&empty_bar[s]), 0));
+              umma2_commit(map_to_cta(smem_u32(&empty_bar[s]), 1));
+              if (kb == KB - 1) {
+                umma2_commit(map_to_cta(smem_u32(&acc_full[buf]), 0));
+                umma2_commit(map_to_cta(smem_u32(&acc_full[buf]), 1));
+              }
+            } else {
+              umma_commit(&empty_bar[s]);
+              if (kb == KB - 1) umma_commit(&acc_full[buf]);
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    const int q = warp & 3, sub = (warp - 2) >> 2;
+    uint32_t tcount = 0;
+    for (int u = walker; u < total; u += n_walkers, ++tcount) {
+      int m0, n0;
+      tile_of(u, &m0, &n0);
+      const uint32_t buf = tcount & 1;
+      mbar_wait(&acc_full[buf], (tcount >> 1) & 1, p.status);
+      tc_fence_after();
+      const uint32_t t_lane = tmem_base + buf * 256 + ((uint32_t)(q * 32) << 16);
+      const int row = m0 + q * 32 + lane, cols = min(t.width, p.n - n0);
+      const bool warp_has_rows = m0 + q * 32 < p.rows;
+      __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (long long)row * p.y_row + n0;
+      const __nv_bfloat16* resid = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + (long long)row * p.resid_row + n0 : nullptr;
+      if (warp_has_rows) {
+#pragma unroll 1
+        for (int c = sub * 32; c < cols; c += 64) {
+          const bool full = c + 32 <= cols;
+          float v[32];
+          tmem_ld_32x32_nowait(t_lane + c, v);
+          uint4 rs[4];
+          const bool wide = full && t.wide_y;
+          if (resid && wide && row < p.rows) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rs[i] = *reinterpret_cast<const uint4*>(resid + c + 8 * i);
+          }
+          tmem_ld_wait();
+          if (p.bias) {
+            const float* b = p.bias + n0 + c;
+            if (full && t.wide_bias) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float4 f = __ldg(reinterpret_cast<const float4*>(b) + i);
+                v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (c + i < cols) v[i] += __ldg(b + i);
+            }
+          }
+          activate(v, p.act);
+          if (row < p.rows) {
+            if (wide) {
+              if (resid) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&rs[i]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float2 f = __bfloat1622float2(h[e]);
+                    v[8 * i + 2 * e] += f.x;
+                    v[8 * i + 2 * e + 1] += f.y;
+                  }
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(y + c)[i] = pack8_bf16(v + 8 * i);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (c + i < cols) {
+                  float o = v[i];
+                  if (resid) o += __bfloat162float(resid[c + i]);
+                  y[c + i] = __float2bfloat16_rn(o);
+                }
+            }
+          }
+          __syncwarp();
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) mbar_arrive_cluster(map_to_cta(smem_u32(&acc_empty[buf]), 0));
+        else mbar_arrive(&acc_empty[buf]);
+      }
+    }
+  }
+  tc_fence_before();
+  if (PAIR) cluster_sync_relaxed(); else __syncthreads();      // nobody frees tensor memory its partner's MMAs may still use
+  if (warp == 1) {
+    if (PAIR) tmem_dealloc2(*tmem_slot, 512);
+    else tmem_dealloc(*tmem_slot, 512);
+  }
+}
+
+// Tile width and form: waves of tiles times what a 64-element k-block takes an SM (the tensor pipe's cycles, or the operand bytes
+// at 64 a cycle), plus the finishing pass of the last tile.
+struct Form { int pair, width; };
+Form pick_form(int rows, int n, int k) {
+  const int m_tiles = (rows + BM - 1) / BM, KB = (k + BK - 1) / BK, x_rows = rows < BM ? (rows + 7) / 8 * 8 : BM;
+  Form best{0, 16};
+  float least = 1e30f;
+  for (int pair = 0; pair <= (m_tiles > 1 ? 1 : 0); ++pair)
+    for (int width = pair ? 32 : 16; width <= 256; width += pair ? 32 : 16) {
+      const int units = (n + width - 1) / width * (pair ? (m_tiles + 1) / 2 : m_tiles), slots = pair ? kSms / 2 : kSms;
+      const float waves = (float)((units + slots - 1) / slots);
+      const float mma = 4.f * fmaxf(48.f, 129.f * (float)width / 256.f);
+      const float feed = (float)(x_rows * 128 + (pair ? width / 2 : width) * 128) / 64.f;
+      const float cycles = waves * (float)KB * fmaxf(mma, feed) + 6.f * (float)width;
+      if (cycles < least) { least = cycles; best = Form{pair, width}; }
+    }
+  return best;
+}
+}  // namespace
+
+cudaError_t launch_linear_tc(const LinearParams& p, cudaStream_t st) {
+  const Form f = pick_form(p.rows, p.n, p.k);
+  const int m_tiles = (p.rows + BM - 1) / BM;
+  TileWalk t = {};
+  t.width = f.width;
+  t.x_rows = !f.pair && p.rows < BM ? (p.rows + 7) / 8 * 8 : BM;
+  t.n_tiles = (p.n + f.width - 1) / f.width;
+  t.m_units = f.pair ? (m_tiles + 1) / 2 : m_tiles;
+  const long long tile_bytes = (long long)f.width * p.k * 2;
+  t.n_group = (int)(kGroupBytes / tile_bytes > 0 ? kGroupBytes / tile_bytes : 1);
+  auto aligned = [](const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; };
+  t.wide_y = aligned(p.y) && p.y_row % 8 == 0 && (!p.resid || (aligned(p.resid) && p.resid_row % 8 == 0));
+  t.wide_bias = aligned(p.bias);
+  // (one row, one output: no stride of its own)
+  const uint64_t k8 = ((uint64_t)p.k + 7) / 8 * 8;
+  CUtensorMap mx, mw;
+  if (!make_map_strided(&mx, p.x, p.rows, p.k, p.rows == 1 ? k8 : p.x_row, t.x_rows) ||
+      !make_map_strided(&mw, p.w, p.n, p.k, p.n == 1 ? k8 : p.w_row, f.pair ? f.width / 2 : f.width))
+    return cudaErrorInvalidValue;
+  const long long units = (long long)t.n_tiles * t.m_units;
+  static std::atomic<unsigned long long> done1{0}, done2{0};
+  if (f.pair) {
+    if (cudaError_t e = ensure_dyn_smem(linear_tc_kernel<true>, SMEM_TOTAL, done2); e != cudaSuccess) return e;
+    return launch_pdl_xz(linear_tc_kernel<true>, dim3(2 * (unsigned)(units < kSms / 2 ? units : kSms / 2)), dim3(kThreads), SMEM_TOTAL, st,
+                         2, 1, mx, mw, p, t);
+  }
+  if (cudaError_t e = ensure_dyn_smem(linear_tc_kernel<false>, SMEM_TOTAL, done1); e != cudaSuccess) return e;
+  return launch_pdl(linear_tc_kernel<false>, dim3((unsigned)(units < kSms ? units : kSms)), dim3(kThreads), SMEM_TOTAL, st, 1, mx, mw, p, t);
+}
+
+}  // namespace dare

@@ -126,6 +126,11 @@ cudaError_t launch_attention_tc(const KvMaps& maps, const AttnParams& p, cudaStr
 // The W tensor maps must have a box of bn rows.
 // Row-major bf16 matrix [rows, cols] as a TMA tensor map with a box of 64 columns x box_rows rows, 128-byte swizzle.
 bool make_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
+// The same with rows further apart than they are long (row_stride elements, a multiple of 8; cols need not be one).
+bool make_map_strided(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t row_stride, uint32_t box_rows);
+// Three dimensions, cols innermost; strides in elements (multiples of 8), box 64 columns x box1 x box2.
+bool make_map_3d(CUtensorMap* m, const void* base, uint64_t cols, uint64_t dim1, uint64_t dim2, uint64_t stride1, uint64_t stride2,
+                 uint32_t box1, uint32_t box2);
 
 // Two-CTA MMAs (pairs of row tiles share their W tile: a third less operand traffic from the L2 per CTA) pay where
 // the main loop is bound by that traffic: launches of at most four row tiles, or of about one wave.  Launches of

@@ -20,6 +20,7 @@ F32, BF16 = 0, 1
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 ROPE_SCALE = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
 ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 
 class LayerConfig(C.Structure):
@@ -59,6 +60,20 @@ class RopeApply(C.Structure):
                 ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("transpose", C.c_int32),
                 ("pos_begin", C.c_int32), ("x_token", C.c_int64), ("x_head", C.c_int64), ("y_token", C.c_int64),
                 ("y_head", C.c_int64), ("table_positions", C.c_int64)]
+
+
+class LinearConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int32),
+                ("out_features", C.c_int32), ("activation", C.c_int32), ("reserved", C.c_int32), ("x_row", C.c_int64),
+                ("w_row", C.c_int64), ("resid_row", C.c_int64), ("y_row", C.c_int64)]
+
+
+class AttentionConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("batch", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float),
+                ("q_rows", C.c_int64), ("k_rows", C.c_int64), ("q_token", C.c_int64), ("q_head", C.c_int64),
+                ("k_token", C.c_int64), ("k_head", C.c_int64), ("v_token", C.c_int64), ("v_head", C.c_int64),
+                ("o_token", C.c_int64), ("o_head", C.c_int64)]
 
 
 class DareError(RuntimeError):
@@ -119,6 +134,9 @@ def _load():
         "dare_select_compact_static": (C.c_int, [vp, C.c_int64, f32, vp, vp, vp]),
         "dare_rope_table": (C.c_int, [C.POINTER(RopeConfig), vp, C.c_int64, vp]),
         "dare_rope": (C.c_int, [C.POINTER(RopeApply), vp, vp, vp, vp, vp, vp]),
+        "dare_linear": (C.c_int, [C.POINTER(LinearConfig), vp, vp, vp, vp, vp, vp, vp]),
+        "dare_attention_workspace_bytes": (sz, [C.POINTER(AttentionConfig)]),
+        "dare_attention": (C.c_int, [C.POINTER(AttentionConfig), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -293,6 +311,21 @@ def dare_rope(cfg: RopeApply, x_ptr, positions_ptr, table_ptr, y_ptr, status_ptr
     return _lib.dare_rope(C.byref(cfg) if cfg is not None else None, x_ptr, positions_ptr, table_ptr, y_ptr, status_ptr, stream)
 
 
+def dare_linear(cfg: LinearConfig, x_ptr, w_ptr, bias_ptr, resid_ptr, y_ptr, status_ptr=None, stream=0) -> int:
+    return _lib.dare_linear(C.byref(cfg) if cfg is not None else None, x_ptr, w_ptr, bias_ptr, resid_ptr, y_ptr, status_ptr,
+                            stream)
+
+
+def dare_attention_workspace_bytes(cfg: AttentionConfig) -> int:
+    return _lib.dare_attention_workspace_bytes(C.byref(cfg) if cfg is not None else None)
+
+
+def dare_attention(cfg: AttentionConfig, q_ptr, k_ptr, v_ptr, q_begin_ptr, k_begin_ptr, k_len_ptr, out_ptr, lse_ptr, workspace_ptr,
+                   workspace_bytes, status_ptr=None, stream=0) -> int:
+    return _lib.dare_attention(C.byref(cfg) if cfg is not None else None, q_ptr, k_ptr, v_ptr, q_begin_ptr, k_begin_ptr,
+                               k_len_ptr, out_ptr, lse_ptr, workspace_ptr, workspace_bytes, status_ptr, stream)
+
+
 def dare_kernel_slot_name(slot: int) -> str:
     return _lib.dare_kernel_slot_name(slot).decode()
 
@@ -426,6 +459,68 @@ def rope(x, table, positions=None, layout=ROPE_LAYOUT["half"], transpose=False, 
     if st != OK:
         raise DareError(st, "dare_rope")
     return out
+
+
+def linear(x, w, bias=None, act=ACT["none"], resid=None, out=None, status=None):
+    """act(x w^T + bias) + resid: x [..., in_features], w [out_features, in_features] (as the layer's weights), bias float32
+    [out_features], resid [..., out_features].  Rows may be strided; out may be resid."""
+    import torch
+    dt = _dtype_of(torch, x)
+    _same_device(x, w, bias, resid, out, status)
+    _check(w.dim() == 2 and w.dtype == x.dtype and w.shape[1] == x.shape[-1] and (w.stride(1) == 1 or w.shape[1] == 1),
+           "w: [out_features, in_features] of x's type, its rows' elements side by side")
+    n, k = w.shape
+    _check(bias is None or (bias.dtype == torch.float32 and bias.shape == (n,) and bias.is_contiguous()),
+           "bias: contiguous float32 [out_features] expected")
+    x2 = x if x.dim() == 2 else x.reshape(-1, k)
+    _check(x2.stride(1) == 1 or k == 1, "the elements of a row of x have to lie side by side")
+    shape = x.shape[:-1] + (n,)
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    for t in (resid, out):
+        _check(t is None or (t.shape == shape and t.dtype == x.dtype), "resid, out: [..., out_features] of x's type expected")
+    y2, r2 = (t if t is None or t.dim() == 2 else t.view(-1, n) for t in (out, resid))
+    _check((y2.stride(1) == 1 or n == 1) and (r2 is None or r2.stride(1) == 1 or n == 1),
+           "the elements of a row of resid and out have to lie side by side")
+    cfg = LinearConfig(C.sizeof(LinearConfig), dt, x2.shape[0], k, n, act, 0, x2.stride(0), w.stride(0),
+                       r2.stride(0) if r2 is not None else 0, y2.stride(0))
+    with _on_device(torch, x.device):
+        st = dare_linear(cfg, x2.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(r2), y2.data_ptr(), _ptr(status),
+                         _current_stream(torch, x.device))
+    if st != OK:
+        raise DareError(st, "dare_linear")
+    return out
+
+
+def attention(q, k, v, q_begin, k_begin, k_len=None, causal=False, scale=None, out=None, return_lse=False, status=None):
+    """Softmax attention over packed sequences: q [q_rows, n_heads, head_dim], k and v [k_rows, n_kv_heads, head_dim] (any row and
+    head strides); q_begin int32 [batch + 1], k_begin int32 [batch + 1] or, with k_len int32 [batch], [batch].  scale: None for
+    head_dim^-0.5.  -> out, or (out, lse float32 [q_rows, n_heads])."""
+    import torch
+    dt = _dtype_of(torch, q)
+    _same_device(q, k, v, q_begin, k_begin, k_len, out, status)
+    _check(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype == v.dtype and q.shape[2] == k.shape[2],
+           "q: [rows, heads, head_dim], k and v: [rows, kv heads, head_dim] of one type expected")
+    _check(q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1, "a head's elements have to lie side by side")
+    batch = q_begin.shape[0] - 1
+    for t, n in ((q_begin, batch + 1), (k_begin, batch if k_len is not None else batch + 1), (k_len, batch)):
+        _check(t is None or (t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.shape[0] >= n),
+               "q_begin, k_begin, k_len: contiguous int32 [batch + 1], [batch + 1] (with k_len: [batch]), [batch] expected")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1, "out: as q")
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
+    cfg = AttentionConfig(C.sizeof(AttentionConfig), dt, batch, q.shape[1], k.shape[1], q.shape[2], 1 if causal else 0,
+                          q.shape[2] ** -0.5 if scale is None else scale, q.shape[0], k.shape[0], q.stride(0), q.stride(1),
+                          k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.stride(0), out.stride(1))
+    nbytes = dare_attention_workspace_bytes(cfg)
+    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+    with _on_device(torch, q.device):
+        st = dare_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_begin.data_ptr(), k_begin.data_ptr(), _ptr(k_len),
+                            out.data_ptr(), _ptr(lse), work.data_ptr(), nbytes, _ptr(status), _current_stream(torch, q.device))
+    if st != OK:
+        raise DareError(st, "dare_attention")
+    return (out, lse) if return_lse else out
 
 
 class Layer:

@@ -55,3 +55,48 @@ def test_rope(dare):
     for kw in (dict(x=P + 1), dict(y=R + 1), dict(t=Q + 4), dict(pos=S + 2)):
         assert call(good, **kw) == dare.ERR_ALIGN, kw
     assert call(_with(good, tokens=0), x=None) == dare.OK
+
+
+def test_attention(dare):
+    good = dare.AttentionConfig(C.sizeof(dare.AttentionConfig), dare.BF16, 2, 8, 2, 128, 1, 0.1, 16, 64, 1024, 128, 256, 128, 256, 128,
+                                1024, 128)
+    need = dare.dare_attention_workspace_bytes(good)
+    assert need > 0
+    W = 0x900000
+
+    def call(c, q=P, k=Q, v=R, qb=S, kb=S + 64, kl=None, out=0x50000, lse=None, work=W, nbytes=need):
+        return dare.dare_attention(c, q, k, v, qb, kb, kl, out, lse, work, nbytes)
+
+    assert call(None) == dare.ERR_INVALID_ARG and dare.dare_attention_workspace_bytes(None) == 0
+    inf, nan = float("inf"), float("nan")
+    for kw in (dict(struct_size=4), dict(dtype=9), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf)):
+        assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
+    for kw in (dict(batch=0), dict(batch=65537), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(head_dim=48),
+               dict(q_rows=-1), dict(q_rows=(1 << 24) + 1), dict(k_rows=-1), dict(k_rows=1 << 31), dict(k_token=-1), dict(v_head=1 << 38),
+               dict(o_head=127), dict(o_token=127), dict(q_rows=1 << 24, n_heads=512)):
+        assert call(_with(good, **kw)) == dare.ERR_SHAPE and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(qb=None), dict(kb=None), dict(out=None), dict(work=None)):
+        assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
+    for kw in (dict(q=P + 1), dict(k=Q + 1), dict(v=R + 1), dict(out=0x50001), dict(qb=S + 2), dict(kb=S + 2), dict(kl=S + 2),
+               dict(lse=S + 2), dict(work=W + 8)):
+        assert call(good, **kw) == dare.ERR_ALIGN, kw
+    assert call(good, nbytes=need - 1) == dare.ERR_WORKSPACE
+    assert call(_with(good, q_rows=0), q=None) == dare.OK
+
+
+def test_linear(dare):
+    good = dare.LinearConfig(C.sizeof(dare.LinearConfig), dare.BF16, 4, 64, 32, 0, 0, 64, 64, 32, 32)
+    call = lambda c, x=P, w=Q, b=None, r=None, y=R: dare.dare_linear(c, x, w, b, r, y)
+    assert call(None) == dare.ERR_INVALID_ARG
+    for kw in (dict(struct_size=1), dict(dtype=3), dict(activation=5), dict(activation=-1), dict(reserved=1)):
+        assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG, kw
+    for kw in (dict(rows=-1), dict(rows=(1 << 24) + 1), dict(in_features=0), dict(in_features=(1 << 20) + 1), dict(out_features=0),
+               dict(out_features=(1 << 24) + 1), dict(rows=1 << 24, out_features=1 << 16), dict(x_row=-1), dict(w_row=1 << 38),
+               dict(y_row=31), dict(resid_row=-1)):
+        assert call(_with(good, **kw)) == dare.ERR_SHAPE, kw
+    for kw in (dict(x=None), dict(w=None), dict(y=None)):
+        assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
+    assert call(_with(good, resid_row=40), r=R) == dare.ERR_INVALID_ARG                     # resid is y with another stride
+    for kw in (dict(x=P + 1), dict(w=Q + 1), dict(y=R + 1), dict(b=S + 2), dict(r=S + 1)):
+        assert call(good, **kw) == dare.ERR_ALIGN, kw
+    assert call(_with(good, rows=0), x=None) == dare.OK
