@@ -8,7 +8,7 @@ using namespace dare;
 namespace {
 
 constexpr int kMaxHeads = 1024;
-constexpr int kMinUnits = 2;         // units of kUnitKeys keys that a share has at least
+constexpr int kMinUnitsTc = 2, kMinUnitsSimt = 1;    // units of kUnitKeys keys that a share has at least
 
 bool valid_config(const dare_attention_config_t* c) {
   if (!c || c->struct_size != sizeof(dare_attention_config_t)) return false;
@@ -32,7 +32,7 @@ bool shape_ok(const dare_attention_config_t* c) {
   return true;
 }
 bool tc_types(const dare_attention_config_t* c) { return c->dtype == DARE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }
-size_t part_bytes(int rows, int head_dim) { return (size_t)2 * kSms * rows * (head_dim * sizeof(float) + sizeof(float2)); }
+size_t part_rows(bool tc) { return (size_t)2 * (tc ? kSms * kTcRows : kSimtCtas * kSimtRows); }      // two slots a CTA
 
 }  // namespace
 
@@ -40,7 +40,7 @@ extern "C" {
 
 size_t dare_attention_workspace_bytes(const dare_attention_config_t* c) {
   if (!valid_config(c) || !shape_ok(c)) return 0;
-  return part_bytes(tc_types(c) ? kTcRows : kSimtRows, c->head_dim);
+  return part_rows(tc_types(c)) * (c->head_dim * sizeof(float) + sizeof(float2));
 }
 
 dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, const void* k, const void* v, const int32_t* q_begin,
@@ -65,8 +65,6 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   p.q_rows = c->q_rows; p.k_rows = c->k_rows;
   p.batch = c->batch; p.n_heads = c->n_heads; p.kv_heads = c->n_kv_heads; p.group = c->n_heads / c->n_kv_heads; p.causal = c->causal;
   p.scale_log2 = c->scale * 1.4426950408889634f;
-  p.n_ctas = kSms;
-  p.min_units = kMinUnits;
 
   // The tensor-core kernel reads k and v through TMA (16-byte aligned rows and heads with strides of their own), q and out by 16
   // bytes.
@@ -77,8 +75,10 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   const bool tc = tc_types(c) && c->k_rows > 0 && !low(q, 15u) && !low(k, 15u) && !low(v, 15u) && !low(out, 15u) && eights(c->q_token) &&
                   eights(c->q_head) && eights(c->o_token) && eights(c->o_head) && tma(c->k_token, c->k_head) && tma(c->v_token, c->v_head);
   const int rows = tc ? kTcRows : kSimtRows;
+  p.n_ctas = tc ? kSms : kSimtCtas;
+  p.min_units = tc ? kMinUnitsTc : kMinUnitsSimt;
   p.part_ml = reinterpret_cast<float2*>(workspace);
-  p.part_o = reinterpret_cast<float*>(p.part_ml + (size_t)2 * kSms * rows);
+  p.part_o = reinterpret_cast<float*>(p.part_ml + part_rows(tc));
 
   cudaError_t e;
   if (tc) {

@@ -10,11 +10,11 @@ using namespace ptx;
 namespace {
 
 // ------------------------------------------------------------------------------------------------ CUDA cores
-// A CTA walks the segments of its share with tiles of 32 rows; four groups of 128 threads take every fourth block of BKV keys and
+// A CTA walks the segments of its share with tiles of 32 rows; two groups of 128 threads take every second block of BKV keys and
 // are merged at the end of a segment.  A thread owns 4 rows: scores of BKV / 16 keys each, then HD / 16 columns of the output each;
 // the 16 lanes of a half-warp share their rows, so the softmax is shuffles and the weights pass through shared memory inside the
-// half-warp.  Everything in fp32.  Bound by the FMA pipe and the shared-memory reads that feed it (8 16-byte reads to 64 FMAs).
-constexpr int BQ = kSimtRows, KG = 4, GROUP = 128, kThreads = KG * GROUP;
+// half-warp.  Two CTAs an SM, so that one multiplies while the other is between two segments.  Everything in fp32.  Bound by the FMA pipe and the shared-memory reads that feed it (8 16-byte reads to 64 FMAs).
+constexpr int BQ = kSimtRows, KG = 2, GROUP = 128, kThreads = KG * GROUP;
 template <int HD>
 struct Sm {
   static constexpr int BKV = HD == 256 ? 16 : (HD == 128 ? 32 : 64), JN = BKV / 16;
@@ -23,7 +23,7 @@ struct Sm {
   static constexpr int BUF = BKV * KP + BKV * HD;
   static constexpr int Q_OFF = 0, P_OFF = BQ * KP, KV_OFF = P_OFF + KG * BQ * PP, FLOATS = KV_OFF + KG * BUF;
   static constexpr int BYTES = FLOATS * 4;
-  static_assert(BYTES <= 226 * 1024 && BQ * HD + 2 * BQ <= BUF, "shared memory; a group's result over its buffer");
+  static_assert(BYTES <= 112 * 1024 && BQ * HD + 2 * BQ <= BUF, "shared memory; a group's result over its buffer");
 };
 
 // four elements of a row as fp32
@@ -44,7 +44,7 @@ __device__ __forceinline__ float4 load4(const T* src, bool wide) {
 }
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedParams p, const bool wide) {
+__global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedParams p, const bool wide) {
   using S = Sm<HD>;
   constexpr int BKV = S::BKV, JN = S::JN, KP = S::KP, PP = S::PP, VW = S::VW, NC = S::NC;
   extern __shared__ __align__(16) float sm[];
@@ -60,9 +60,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
   const T* q = reinterpret_cast<const T*>(p.q);
   const T* kg = reinterpret_cast<const T*>(p.k);
   const T* vg = reinterpret_cast<const T*>(p.v);
+  Line<BQ, true> line(p);                        // (used by warp 0)
   if (tid < 32) {
-    long long total = 0;
-    const long long per = share_units<BQ>(p, &total), begin = (long long)blockIdx.x * per;
+    const long long total = line.total(), per = share_units<BQ>(p, total), begin = (long long)blockIdx.x * per;
     if (tid == 0) {
       share_sh[0] = begin;
       share_sh[1] = begin + per < total ? begin + per : total;
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
   for (long long u = share_begin; u < share_end;) {
     if (tid < 32) {
       Place pl;
-      if (find_place<BQ, true>(p, u, &pl, nullptr) && tid == 0) pl_sh = pl;
+      if (line.find(u, &pl) && tid == 0) pl_sh = pl;
     }
     __syncthreads();
     const Place pl = pl_sh;
@@ -95,34 +95,56 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
     int seen[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) seen[i] = keys_seen(p, pl.s, row_at(p, pl, row0 + min(ty + 8 * i, rows - 1)).query);
-    float m[4], l[4], acc[4][NC * VW];
+    float m[4], l[4];
+    float2 acc[4][NC * VW / 2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
-      for (int e = 0; e < NC * VW; ++e) acc[i][e] = 0.f;
+      for (int e = 0; e < NC * VW / 2; ++e) acc[i][e] = make_float2(0.f, 0.f);
     }
     __syncthreads();
-    for (int kb = key0 + grp * BKV; kb < key1; kb += KG * BKV) {
-      const int keys = min(BKV, key1 - kb);
-      for (int i = lt; i < BKV * (HD / 4); i += GROUP) {
-        const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        if (r < keys) {
-          const long long row = (long long)pl.s.k0 + kb + r;
-          a = load4(kg + row * p.k_token + pl.h * p.k_head + d, wide);
-          b = load4(vg + row * p.v_token + pl.h * p.v_head + d, wide);
+    // A group's next keys come while it multiplies weights and values, its next values while it works out scores (float32: asynchronous
+    // copies, two groups of them in flight).
+    auto fetch = [&](float* dst, int pitch, const T* src, long long token, long long head, int kb) {
+      constexpr int N = BKV * (HD / 4) / GROUP;
+      const T* base = src + (long long)pl.s.k0 * token + pl.h * head;
+      float4 x[sizeof(T) == 4 ? 1 : N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int e = lt + i * GROUP, r = e / (HD / 4), d = (e % (HD / 4)) * 4;
+        const bool there = kb + r < key1;                 // (else zeros: what lies there may be anything)
+        const T* at = base + (there ? (long long)(kb + r) * token + d : 0);
+        if constexpr (sizeof(T) == 4) {
+          if (wide) cp_async_16(smem_u32(dst + r * pitch + d), at, there ? 16u : 0u);
+          else *reinterpret_cast<float4*>(dst + r * pitch + d) = there ? load4(at, false) : make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          x[i] = there ? load4(at, wide) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        *reinterpret_cast<float4*>(ks + r * KP + d) = a;
-        *reinterpret_cast<float4*>(vs + r * HD + d) = b;
       }
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(GROUP) : "memory");
-      float s[4][JN];
+      if constexpr (sizeof(T) != 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int e = lt + i * GROUP, r = e / (HD / 4), d = (e % (HD / 4)) * 4;
+          *reinterpret_cast<float4*>(dst + r * pitch + d) = x[i];
+        }
+      }
+      cp_async_commit();
+    };
+    auto fetch_k = [&](int kb) { if (kb < key1) fetch(ks, KP, kg, p.k_token, p.k_head, kb); else cp_async_commit(); };
+    auto fetch_v = [&](int kb) { if (kb < key1) fetch(vs, HD, vg, p.v_token, p.v_head, kb); else cp_async_commit(); };
+    auto group_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(GROUP) : "memory"); };
+    fetch_k(key0 + grp * BKV);
+    fetch_v(key0 + grp * BKV);
+    for (int kb = key0 + grp * BKV; kb < key1; kb += KG * BKV) {
+      cp_async_wait<1>();                                 // the keys are here
+      group_sync();
+      float2 s2[4][JN];                                   // sums over even and over odd elements
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < JN; ++j) s[i][j] = 0.f;
+        for (int j = 0; j < JN; ++j) s2[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
       for (int d = 0; d < HD; d += 4) {
         float4 a[4], b[JN];
@@ -134,19 +156,19 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < JN; ++j) {
-            s[i][j] = fmaf(a[i].x, b[j].x, s[i][j]);
-            s[i][j] = fmaf(a[i].y, b[j].y, s[i][j]);
-            s[i][j] = fmaf(a[i].z, b[j].z, s[i][j]);
-            s[i][j] = fmaf(a[i].w, b[j].w, s[i][j]);
+            s2[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), s2[i][j]);
+            s2[i][j] = __ffma2_rn(make_float2(a[i].z, a[i].w), make_float2(b[j].z, b[j].w), s2[i][j]);
           }
       }
+      group_sync();                                       // everybody is through with the keys
+      fetch_k(kb + KG * BKV);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float top = -INFINITY;
+        float top = -INFINITY, s[JN];
 #pragma unroll
         for (int j = 0; j < JN; ++j) {
-          s[i][j] = kb + tx + 16 * j < min(seen[i], key1) ? s[i][j] * p.scale_log2 : -INFINITY;
-          top = fmaxf(top, s[i][j]);
+          s[j] = kb + tx + 16 * j < min(seen[i], key1) ? (s2[i][j].x + s2[i][j].y) * p.scale_log2 : -INFINITY;
+          top = fmaxf(top, s[j]);
         }
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -155,15 +177,16 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
         m[i] = m_new;
         l[i] *= alpha;
 #pragma unroll
-        for (int e = 0; e < NC * VW; ++e) acc[i][e] *= alpha;
+        for (int e = 0; e < NC * VW / 2; ++e) acc[i][e] = __fmul2_rn(acc[i][e], make_float2(alpha, alpha));
 #pragma unroll
         for (int j = 0; j < JN; ++j) {
-          const float w = exp2f(s[i][j] - base);
+          const float w = exp2f(s[j] - base);
           l[i] += w;                                                     // (this lane's keys; the lanes are added up at the end)
           ps[(ty + 8 * i) * PP + tx + 16 * j] = w;
         }
       }
-      __syncwarp();
+      cp_async_wait<1>();                                 // the values are here
+      group_sync();
 #pragma unroll 2
       for (int j = 0; j < BKV; j += 4) {
         float4 w[4];
@@ -171,27 +194,25 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
         for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(ps + (ty + 8 * i) * PP + j);
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
-          float v[NC * VW];
+          float2 v[NC * VW / 2];
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
             const float* src = vs + (j + jj) * HD + c * 16 * VW + tx * VW;
-#pragma unroll
-            for (int e = 0; e < VW; e += 2) {
-              const float2 t = *reinterpret_cast<const float2*>(src + e);
-              v[c * VW + e] = t.x;
-              v[c * VW + e + 1] = t.y;
-            }
+            if constexpr (VW == 4) *reinterpret_cast<float4*>(v + 2 * c) = *reinterpret_cast<const float4*>(src);
+            else v[c] = *reinterpret_cast<const float2*>(src);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float wj = jj == 0 ? w[i].x : (jj == 1 ? w[i].y : (jj == 2 ? w[i].z : w[i].w));
 #pragma unroll
-            for (int e = 0; e < NC * VW; ++e) acc[i][e] = fmaf(wj, v[e], acc[i][e]);
+            for (int e = 0; e < NC * VW / 2; ++e) acc[i][e] = __ffma2_rn(make_float2(wj, wj), v[e], acc[i][e]);
           }
         }
       }
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(GROUP) : "memory");
+      group_sync();                                       // everybody is through with the values
+      fetch_v(kb + KG * BKV);
     }
+    cp_async_wait<0>();
     // ---- the groups' results over their buffers, merged by everybody
     float* res = ks;
 #pragma unroll
@@ -206,7 +227,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_simt_kernel(const PackedPa
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int e = 0; e < VW; ++e) res[r * HD + c * 16 * VW + tx * VW + e] = acc[i][c * VW + e];
+        for (int e = 0; e < VW / 2; ++e)
+          *reinterpret_cast<float2*>(res + r * HD + c * 16 * VW + tx * VW + 2 * e) = acc[i][c * (VW / 2) + e];
     }
     __syncthreads();
     for (int i = tid; i < rows * (HD / 4); i += kThreads) {
@@ -256,50 +278,48 @@ cudaError_t launch_simt_as(const PackedParams& p, cudaStream_t st) {
 
 // ------------------------------------------------------------------------------------------------ merge
 // o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the shares that hold keys of the row's pair, in the order of the keys (so the
-// result does not depend on which CTA was first).  One CTA a pair; a thread has four columns of a row.  A pair that lies in one
-// share was written by it.
+// result does not depend on which CTA was first).  A CTA has 512 / HD rows of a pair, a thread four columns of one: with one CTA a
+// pair its rows came one after the other, 30 us for tiles of 128 rows.  A pair that lies in one share was written by it.
+constexpr int kCombineThreads = 128;     // (beside a CTA of the kernel before: it waits for that one's end on the SM already)
 template <typename T, int HD, int ROWS>
-__global__ void __launch_bounds__(256) packed_combine_kernel(const PackedParams p) {
+__global__ void __launch_bounds__(kCombineThreads) packed_combine_kernel(const PackedParams p) {
+  constexpr int kRows = kCombineThreads / (HD / 4);       // rows of this CTA
   __shared__ Place pl_sh;
   __shared__ long long per_sh;
   __shared__ int more_sh;
-  pdl_wait();
-  pdl_launch_dependents();
+  // (the lengths are inputs: complete before the kernel in front let this one start)
   if (threadIdx.x < 32) {
-    // (blockIdx.x counts pairs: looked up by pair, the unit it begins at by its place among the units)
-    long long total = 0, base_units = 0, base_pairs = 0;
+    // blockIdx.x counts pairs: looked up in the line of pairs, the unit it begins at by the units before it
     const int lane = threadIdx.x;
-    const long long per = share_units<ROWS>(p, &total), u = blockIdx.x;
+    Line<ROWS, true> line(p);
+    const long long per = share_units<ROWS>(p, line.total());
+    line.rewind();
+    long long pairs_before = 0;
     bool found = false;
-    for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {
-      const int b = b0 + lane;
-      SeqGeom s{0, 0, 0, 0};
-      if (b < p.batch) s = seq_geom(p, b);
-      const long long pairs = (((long long)s.nq * p.group + ROWS - 1) / ROWS) * p.kv_heads;
-      const int units = max(1, (s.n + kUnitKeys - 1) / kUnitKeys);
-      long long inc = pairs, inc_u = pairs * units;
+    do {
+      const long long pairs = (long long)line.tiles * p.kv_heads;
+      long long inc = pairs;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, inc, o), w = __shfl_up_sync(0xffffffffu, inc_u, o);
-        if (lane >= o) { inc += v; inc_u += w; }
+        const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
       }
-      const unsigned hit = __ballot_sync(0xffffffffu, u < base_pairs + inc);
+      const unsigned hit = __ballot_sync(0xffffffffu, (long long)blockIdx.x < pairs_before + inc);
       if (hit != 0u) {
         const int src = __ffs((int)hit) - 1;
-        const long long pair = u - (base_pairs + __shfl_sync(0xffffffffu, inc - pairs, src));
-        const long long first = base_units + __shfl_sync(0xffffffffu, inc_u - pairs * units, src) +
-                                pair * __shfl_sync(0xffffffffu, units, src);
         Place pl;
-        find_place<ROWS, true>(p, first, &pl, nullptr);
+        line.place(src, line.base + __shfl_sync(0xffffffffu, line.inc - line.mine, src),
+                   (long long)blockIdx.x - (pairs_before + __shfl_sync(0xffffffffu, inc - pairs, src)), &pl);
         if (lane == 0) { pl_sh = pl; per_sh = per; }
         found = true;
       }
-      base_pairs += __shfl_sync(0xffffffffu, inc, 31);
-      base_units += __shfl_sync(0xffffffffu, inc_u, 31);
-    }
+      pairs_before += __shfl_sync(0xffffffffu, inc, 31);
+    } while (!found && line.next());
     if (lane == 0) more_sh = found ? 1 : 0;
   }
   __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
   if (!more_sh) return;
   const Place pl = pl_sh;
   const long long per = per_sh;
@@ -308,34 +328,36 @@ __global__ void __launch_bounds__(256) packed_combine_kernel(const PackedParams 
   const int row0 = pl.tile * ROWS, rows = (int)min((long long)ROWS, (long long)pl.s.nq * p.group - row0);
   // the first share's part is the last of that CTA (unless the share begins with this pair), the others' their first
   auto slot_of = [&](int c) { return 2 * c + (c == c0 && pl.first > c0 * per ? 1 : 0); };
-  for (int i = threadIdx.x; i < rows * (HD / 4); i += 256) {
-    const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
-    float top = -INFINITY;
+  const int r = (int)blockIdx.y * kRows + (int)threadIdx.x / (HD / 4), d = ((int)threadIdx.x % (HD / 4)) * 4;
+  if (r >= rows) return;
+  float top = -INFINITY;
 #pragma unroll 8
-    for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(p.part_ml + (size_t)slot_of(c) * ROWS + r).x);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-      const size_t at = (size_t)slot_of(c) * ROWS + r;
-      const float2 ml = __ldcg(p.part_ml + at);
-      const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + d));
-      const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
-      o.x = fmaf(a.x, w, o.x); o.y = fmaf(a.y, w, o.y); o.z = fmaf(a.z, w, o.z); o.w = fmaf(a.w, w, o.w);
-      sum = fmaf(ml.y, w, sum);
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const RowAt at = row_at(p, pl, row0 + r);
-    T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d;
-    dst[0] = (T)(o.x * inv); dst[1] = (T)(o.y * inv); dst[2] = (T)(o.z * inv); dst[3] = (T)(o.w * inv);
-    if (p.lse && d == 0)
-      p.lse[(long long)(pl.s.q0 + at.query) * p.n_heads + at.head] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
+  for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(p.part_ml + (size_t)slot_of(c) * ROWS + r).x);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = 0.f;
+#pragma unroll 8
+  for (int c = c0; c <= c1; ++c) {
+    const size_t at = (size_t)slot_of(c) * ROWS + r;
+    const float2 ml = __ldcg(p.part_ml + at);
+    const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + d));
+    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+    o.x = fmaf(a.x, w, o.x); o.y = fmaf(a.y, w, o.y); o.z = fmaf(a.z, w, o.z); o.w = fmaf(a.w, w, o.w);
+    sum = fmaf(ml.y, w, sum);
   }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const RowAt at = row_at(p, pl, row0 + r);
+  T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d;
+  dst[0] = (T)(o.x * inv); dst[1] = (T)(o.y * inv); dst[2] = (T)(o.z * inv); dst[3] = (T)(o.w * inv);
+  if (p.lse && d == 0)
+    p.lse[(long long)(pl.s.q0 + at.query) * p.n_heads + at.head] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
 }
 template <typename T, int HD, int ROWS>
 cudaError_t launch_combine_as(const PackedParams& p, cudaStream_t st) {
-  const long long pairs = ((p.q_rows * p.group) / ROWS + p.batch) * p.kv_heads;
-  return launch_pdl(packed_combine_kernel<T, HD, ROWS>, dim3((unsigned)pairs), dim3(256), 0, st, 1, p);
+  // (no tile has more rows than there are)
+  constexpr int kRows = kCombineThreads / (HD / 4);
+  const long long all = p.q_rows * p.group, pairs = (all / ROWS + p.batch) * p.kv_heads, rows = all < ROWS ? all : ROWS;
+  return launch_pdl(packed_combine_kernel<T, HD, ROWS>, dim3((unsigned)pairs, (unsigned)((rows + kRows - 1) / kRows)),
+                    dim3(kCombineThreads), 0, st, 1, p);
 }
 }  // namespace
 

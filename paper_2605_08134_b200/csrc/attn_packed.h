@@ -72,55 +72,85 @@ struct Place {
   long long first;               // unit of the launch's line where the pair begins
 };
 
-// Pair that holds unit u of the line, found by a warp (all lanes get it); false: u is behind the last one, *total (if given) then
-// is the line's length.  UNITS: a pair counts as its units of keys, else as one.
+__device__ __forceinline__ long long divide(long long a, int b) {       // (64-bit divisions cost ten times as much)
+  return a <= 0x7fffffffll ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
+// The launch's line of pairs, as a warp looks places up in it.  UNITS: a pair counts as its units of keys, else as one.  Lane l holds
+// sequence l of the 32 looked at last, so that with at most 32 sequences the lengths are read once.
 template <int BQ, bool UNITS>
-__device__ __forceinline__ bool find_place(const PackedParams& p, long long u, Place* out, long long* total) {
-  const int lane = threadIdx.x & 31;
-  long long base = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const int b = b0 + lane;
-    SeqGeom s{0, 0, 0, 0};
+struct Line {
+  const PackedParams& p;
+  SeqGeom s;
+  int tiles, units, b0;          // of this lane's sequence; first sequence of the 32
+  long long base, mine, inc;     // units before the 32; of this lane's sequence; up to and with it
+
+  __device__ __forceinline__ explicit Line(const PackedParams& p_) : p(p_) {
+    load(0);
+    base = 0;
+  }
+  __device__ __forceinline__ void load(int first) {
+    const int lane = threadIdx.x & 31, b = first + lane;
+    b0 = first;
+    s = SeqGeom{0, 0, 0, 0};
     if (b < p.batch) s = seq_geom(p, b);
-    const int tiles = (int)(((long long)s.nq * p.group + BQ - 1) / BQ);
-    const int units = UNITS ? max(1, (s.n + kUnitKeys - 1) / kUnitKeys) : 1;
-    const long long mine = (long long)tiles * p.kv_heads * units;
-    long long inc = mine;
+    tiles = (int)(((long long)s.nq * p.group + BQ - 1) / BQ);
+    units = UNITS ? max(1, (s.n + kUnitKeys - 1) / kUnitKeys) : 1;
+    mine = (long long)tiles * p.kv_heads * units;
+    inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long v = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += v;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, u < base + inc);
-    if (hit != 0u) {
-      const int src = __ffs((int)hit) - 1;
-      out->s.q0 = __shfl_sync(0xffffffffu, s.q0, src);
-      out->s.nq = __shfl_sync(0xffffffffu, s.nq, src);
-      out->s.k0 = __shfl_sync(0xffffffffu, s.k0, src);
-      out->s.n = __shfl_sync(0xffffffffu, s.n, src);
-      out->tiles = __shfl_sync(0xffffffffu, tiles, src);
-      out->units = __shfl_sync(0xffffffffu, units, src);
-      const long long begin = base + __shfl_sync(0xffffffffu, inc - mine, src);
-      const long long pair = (u - begin) / out->units;                   // head by head
-      out->h = (int)(pair / out->tiles);
-      const int t = (int)(pair - (long long)out->h * out->tiles);
-      // shares: first, last, second, last but one ... (causal tiles cost in proportion to their place: any two in a row cost
-      // the same); tiles: the longest first
-      out->tile = UNITS ? ((t & 1) ? out->tiles - 1 - (t >> 1) : (t >> 1)) : out->tiles - 1 - t;
-      out->first = begin + pair * out->units;
-      return true;
-    }
-    base += __shfl_sync(0xffffffffu, inc, 31);
   }
-  if (total) *total = base;
-  return false;
-}
+  // next 32 sequences; false: there are none
+  __device__ __forceinline__ bool next() {
+    if (b0 + 32 >= p.batch) return false;
+    base += __shfl_sync(0xffffffffu, inc, 31);
+    load(b0 + 32);
+    return true;
+  }
+  __device__ __forceinline__ void rewind() {
+    if (b0 != 0) load(0);
+    base = 0;
+  }
+  __device__ __forceinline__ long long total() {
+    rewind();
+    while (next()) {}
+    return base + __shfl_sync(0xffffffffu, inc, 31);
+  }
+  // Pair that holds unit u; the same for all lanes.  false: u is behind the last one.
+  __device__ __forceinline__ bool find(long long u, Place* out) {
+    if (u < base) rewind();
+    unsigned hit;
+    while ((hit = __ballot_sync(0xffffffffu, u < base + inc)) == 0u)
+      if (!next()) return false;
+    const int src = __ffs((int)hit) - 1;
+    const long long begin = base + __shfl_sync(0xffffffffu, inc - mine, src);
+    place(src, begin, divide(u - begin, __shfl_sync(0xffffffffu, units, src)), out);
+    return true;
+  }
+  // Pair number `pair` of lane src's sequence, whose units begin at `begin`.
+  __device__ __forceinline__ void place(int src, long long begin, long long pair, Place* out) {
+    out->s.q0 = __shfl_sync(0xffffffffu, s.q0, src);
+    out->s.nq = __shfl_sync(0xffffffffu, s.nq, src);
+    out->s.k0 = __shfl_sync(0xffffffffu, s.k0, src);
+    out->s.n = __shfl_sync(0xffffffffu, s.n, src);
+    out->tiles = __shfl_sync(0xffffffffu, tiles, src);
+    out->units = __shfl_sync(0xffffffffu, units, src);
+    out->h = (int)divide(pair, out->tiles);                            // head by head
+    const int t = (int)(pair - (long long)out->h * out->tiles);
+    // shares: first, last, second, last but one ... (causal tiles cost in proportion to their place: any two in a row cost
+    // the same); tiles: the longest first
+    out->tile = UNITS ? ((t & 1) ? out->tiles - 1 - (t >> 1) : (t >> 1)) : out->tiles - 1 - t;
+    out->first = begin + pair * out->units;
+  }
+};
 // units of a share
 template <int BQ>
-__device__ __forceinline__ long long share_units(const PackedParams& p, long long* total) {
-  Place unused;
-  find_place<BQ, true>(p, 0x7fffffffffffffffll, &unused, total);
-  const long long per = (*total + p.n_ctas - 1) / p.n_ctas;
+__device__ __forceinline__ long long share_units(const PackedParams& p, long long total) {
+  const long long per = divide(total + p.n_ctas - 1, p.n_ctas);
   return per < p.min_units ? p.min_units : per;
 }
 // Row of a tile -> its place in q, out and lse.
@@ -140,5 +170,6 @@ cudaError_t launch_packed_simt(const PackedParams& p, int head_dim, bool bf16, c
 // merges what the shares left (attn_packed.cu); bq: rows of their tiles
 cudaError_t launch_packed_combine(const PackedParams& p, int head_dim, int bq, bool bf16, cudaStream_t st);
 constexpr int kTcRows = 128, kSimtRows = 32;
+constexpr int kSimtCtas = 2 * kSms;             // shares of the CUDA-core kernel: two CTAs an SM
 
 }  // namespace dare

@@ -84,9 +84,12 @@ __device__ __forceinline__ int blocks_seen(const PackedParams& p, const Segment&
 
 // The segment of a share that begins at unit u (shares), or CTA u's pair (tiles); *end: unit behind it.  By a warp.
 template <bool TILES>
-__device__ __forceinline__ bool segment_at(const PackedParams& p, long long u, long long share_begin, long long share_end, Segment* g,
+using WorkLine = Line<TILES ? 2 * BQ : BQ, !TILES>;
+template <bool TILES>
+__device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, long long u, long long share_begin, long long share_end, Segment* g,
                                            long long* end) {
-  if (!find_place<TILES ? 2 * BQ : BQ, !TILES>(p, u, &g->pl, nullptr)) return false;
+  const PackedParams& p = line.p;
+  if (!line.find(u, &g->pl)) return false;
   constexpr int ROWS = TILES ? 2 * BQ : BQ;
   g->row0 = g->pl.tile * ROWS;
   const long long left = (long long)g->pl.s.nq * p.group - g->row0;
@@ -154,23 +157,25 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  // this CTA's part of the launch's line of units (tiles: pair blockIdx.x); warps 0-2 know it
+  // this CTA's part of the launch's line of units (tiles: pair blockIdx.x)
   long long share_begin = blockIdx.x, share_end = (long long)blockIdx.x + 1;
-  if (!TILES && warp <= 2) {
-    long long total = 0;
-    const long long per = share_units<BQ>(p, &total);
+  auto find_share = [&](WorkLine<TILES>& line) {
+    if (TILES) return;
+    const long long total = line.total(), per = share_units<BQ>(p, total);
     share_begin = (long long)blockIdx.x * per;
     share_end = share_begin + per < total ? share_begin + per : total;
-  }
+  };
 
   const int st = warp < 4 ? (warp & 1) : ((warp - 4) >> 2);                  // stream
   if (warp < 2) {
     // ---- producers (tiles: warp 0)
     if (!TILES || warp == 0) {
+      WorkLine<TILES> line(p);
+      find_share(line);
       Segment g;
       long long u = share_begin, next;
       uint32_t cnt = 0;
-      for (; u < share_end && segment_at<TILES>(p, u, share_begin, share_end, &g, &next); u = next) {
+      for (; u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next); u = next) {
         const int n = TILES ? g.n_blk : (g.n_blk - st + 1) / 2;
         for (int j = 0; j < n; ++j, ++cnt) {
           const int slot = (TILES ? 0 : st * RING) + (int)(cnt % RING);
@@ -187,6 +192,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     }
   } else {
     const uint32_t tmem_s = tmem_base + st * 2 * BK, tmem_o = tmem_base + 4 * BK + st * HD;
+    // (warp 2 looks the segments up; the others get them through shared memory)
+    WorkLine<TILES> line(p);
+    if (warp == 2) find_share(line);
     long long u = share_begin, next = 0;
     uint32_t cnt = 0;                        // blocks of this stream so far: score buffer cnt & 1
     uint32_t kcnt = 0;                       // ring position (tiles: blocks of both streams)
@@ -195,7 +203,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
       if (warp == 2) {
         Segment g;
-        const bool more = u < share_end && segment_at<TILES>(p, u, share_begin, share_end, &g, &next);
+        const bool more = u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next);
         u = next;
         if (lane == 0) {
           seg_more = more ? 1 : 0;

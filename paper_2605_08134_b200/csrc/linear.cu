@@ -9,30 +9,37 @@ using namespace ptx;
 
 namespace {
 
-// A warp takes kOut outputs and up to MT rows: its lanes share the k-elements, four a lane and step, and add their sums up at the end,
-// halving the set of sums a lane holds at each step of the exchange.  W is read once for MT rows (blockIdx.x counts groups of rows:
-// CTAs side by side take the same rows of W, which the second finds in the L2).  Every W element a lane has feeds MT multiplications
-// and every x element kOut, so at 16 rows the FMA pipe and the L1 that feeds it are about even (64 cycles against 80 a step).
+// ------------------------------------------------------------------------------------------------ few rows
+// At most four rows: a stream of W.  A warp takes kOut outputs; its lanes share the k-elements, VE (16 bytes of a row that allows it)
+// a lane and step, and add their sums up at the end, halving the set of sums a lane holds at each step of the exchange.  Sums of
+// even and odd k-elements run side by side in packed multiply-adds.
 constexpr int kOut = 4, kWarps = 8, kThreads = kWarps * 32;
 
-template <typename T, bool WIDE>
-__device__ __forceinline__ float4 load4(const T* row, int k, int K) {
-  if constexpr (WIDE) {                                    // (K a multiple of 4: all four or none)
-    if (k >= K) return make_float4(0.f, 0.f, 0.f, 0.f);
-    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(row + k);
-    else {
-      const uint2 raw = *reinterpret_cast<const uint2*>(row + k);
-      const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.x));
-      const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.y));
-      return make_float4(a.x, a.y, b.x, b.y);
+// VE elements of a row from k on as pairs; past K: zeros
+template <typename T, int VE, bool WIDE>
+__device__ __forceinline__ void load_pairs(const T* row, int k, int K, float2 (&v)[VE / 2]) {
+  if (WIDE && k + VE <= K) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < VE / 4; ++i) {
+        const float4 f = *reinterpret_cast<const float4*>(row + k + 4 * i);
+        v[2 * i] = make_float2(f.x, f.y);
+        v[2 * i + 1] = make_float2(f.z, f.w);
+      }
+    } else {
+      uint32_t raw[VE / 2];
+      if constexpr (VE == 8) *reinterpret_cast<uint4*>(raw) = *reinterpret_cast<const uint4*>(row + k);
+      else *reinterpret_cast<uint2*>(raw) = *reinterpret_cast<const uint2*>(row + k);
+#pragma unroll
+      for (int i = 0; i < VE / 2; ++i) v[i] = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw[i]));
     }
+    return;
   }
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (k < K) v.x = (float)row[k];
-  if (k + 1 < K) v.y = (float)row[k + 1];
-  if (k + 2 < K) v.z = (float)row[k + 2];
-  if (k + 3 < K) v.w = (float)row[k + 3];
-  return v;
+#pragma unroll
+  for (int i = 0; i < VE / 2; ++i) {
+    v[i].x = k + 2 * i < K ? (float)row[k + 2 * i] : 0.f;
+    v[i].y = k + 2 * i + 1 < K ? (float)row[k + 2 * i + 1] : 0.f;
+  }
 }
 
 // Sums over the lanes of N values each: afterwards lane l holds max(1, N / 32) of them, the first of which is value *first.
@@ -56,41 +63,41 @@ __device__ __forceinline__ void reduce_lanes(float* v, int* first) {
   }
 }
 
-template <typename T, int MT, bool WIDE>
+template <typename T, int MT, int VE, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int m0 = (int)blockIdx.x * MT;
-  const long long n0 = ((long long)blockIdx.y + (long long)blockIdx.z * gridDim.y) * (kWarps * kOut) + warp * kOut;
+  const long long n0 = (long long)blockIdx.x * (kWarps * kOut) + warp * kOut;
   if (n0 >= p.n) return;
   const T* x[MT];
   const T* w[kOut];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) x[i] = reinterpret_cast<const T*>(p.x) + (long long)min(m0 + i, p.rows - 1) * p.x_row;
+  for (int i = 0; i < MT; ++i) x[i] = reinterpret_cast<const T*>(p.x) + (long long)min(i, p.rows - 1) * p.x_row;
 #pragma unroll
   for (int j = 0; j < kOut; ++j) w[j] = reinterpret_cast<const T*>(p.w) + min(n0 + j, (long long)p.n - 1) * p.w_row;
-  float acc[kOut * MT];
+  float2 sums[kOut * MT];
 #pragma unroll
-  for (int i = 0; i < kOut * MT; ++i) acc[i] = 0.f;
-#pragma unroll 2
-  for (int k = lane * 4; k < p.k; k += 128) {
-    float4 a[kOut];
+  for (int i = 0; i < kOut * MT; ++i) sums[i] = make_float2(0.f, 0.f);
+  constexpr int kUnroll = MT <= 2 ? 4 : 2;
+#pragma unroll kUnroll
+  for (int k = lane * VE; k < p.k; k += 32 * VE) {
+    float2 a[kOut][VE / 2];
 #pragma unroll
-    for (int j = 0; j < kOut; ++j) a[j] = load4<T, WIDE>(w[j], k, p.k);
+    for (int j = 0; j < kOut; ++j) load_pairs<T, VE, WIDE>(w[j], k, p.k, a[j]);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const float4 b = load4<T, WIDE>(x[i], k, p.k);
+      float2 b[VE / 2];
+      load_pairs<T, VE, WIDE>(x[i], k, p.k, b);
 #pragma unroll
-      for (int j = 0; j < kOut; ++j) {
-        float& s = acc[i * kOut + j];
-        s = fmaf(a[j].x, b.x, s);
-        s = fmaf(a[j].y, b.y, s);
-        s = fmaf(a[j].z, b.z, s);
-        s = fmaf(a[j].w, b.w, s);
-      }
+      for (int j = 0; j < kOut; ++j)
+#pragma unroll
+        for (int e = 0; e < VE / 2; ++e) sums[i * kOut + j] = __ffma2_rn(a[j][e], b[e], sums[i * kOut + j]);
     }
   }
+  float acc[kOut * MT];
+#pragma unroll
+  for (int i = 0; i < kOut * MT; ++i) acc[i] = sums[i].x + sums[i].y;
   constexpr int N = kOut * MT, LEFT = N > 32 ? N / 32 : 1;
   int first = 0;
   reduce_lanes<N, 16>(acc, &first);
@@ -105,7 +112,7 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
   activate(v, p.act);
 #pragma unroll
   for (int i = 0; i < LEFT; ++i) {
-    const int m = m0 + (first + i) / kOut, n = (int)n0 + (first + i) % kOut;
+    const int m = (first + i) / kOut, n = (int)n0 + (first + i) % kOut;
     if (m < p.rows && n < p.n) {
       if (p.resid) v[i] += (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n];
       reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)v[i];
@@ -113,32 +120,217 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
   }
 }
 
-template <typename T, int MT>
-cudaError_t launch_rows_as(const LinearParams& p, bool wide, cudaStream_t st) {
-  const long long n_ctas = ((long long)p.n + kWarps * kOut - 1) / (kWarps * kOut), nz = (n_ctas + 65534) / 65535;
-  return launch_pdl(wide ? linear_rows_kernel<T, MT, true> : linear_rows_kernel<T, MT, false>, dim3((unsigned)((p.rows + MT - 1) / MT), (unsigned)((n_ctas + nz - 1) / nz), (unsigned)nz),
-                    dim3(kThreads), 0, st, 1, p);
+template <typename T, int MT, int VE, bool WIDE>
+cudaError_t launch_rows_as(const LinearParams& p, cudaStream_t st) {
+  return launch_pdl(linear_rows_kernel<T, MT, VE, WIDE>, dim3((unsigned)((p.n + kWarps * kOut - 1) / (kWarps * kOut))), dim3(kThreads), 0,
+                    st, 1, p);
 }
+template <typename T, int VE, bool WIDE>
+cudaError_t launch_rows_by(const LinearParams& p, cudaStream_t st) {
+  if (p.rows == 1) return launch_rows_as<T, 1, VE, WIDE>(p, st);
+  if (p.rows == 2) return launch_rows_as<T, 2, VE, WIDE>(p, st);
+  return launch_rows_as<T, 4, VE, WIDE>(p, st);
+}
+
+// ------------------------------------------------------------------------------------------------ tiles
+// More rows: tiles of 8 RM rows x 64 outputs.  Two groups of 128 threads take every second 16 of a step's 32 k-elements; a thread owns
+// RM rows x 4 outputs and reads four k-elements of each at a time.  Operands lie in shared memory row by row, three steps deep.
+// Few tiles: the k-elements are split over a cluster of up to eight CTAs (blockIdx.z); each leaves its sums in shared memory and
+// finishes its part of the rows from everybody's, in the order of the k-elements.  Bound by the FMA pipe and the shared-memory reads
+// that feed it (RM + 8 wavefronts to 16 RM multiply-adds of a warp).
+constexpr int TN = 64, TK = 32, kPitch = TK + 4, kTileStages = 3, kGroup = 128, kTileThreads = 2 * kGroup;
+template <int RM>
+struct Tile {
+  static constexpr int BM = 8 * RM, STAGE = (BM + TN) * kPitch;                 // floats
+  static constexpr int SUMS = BM * (TN + 4);
+  static constexpr int FLOATS = kTileStages * STAGE > 2 * SUMS ? kTileStages * STAGE : 2 * SUMS;
+  static constexpr int BYTES = FLOATS * 4;
+};
+
+template <typename T, int RM, bool WIDE>
+__global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const LinearParams p, const int k_part) {
+  using S = Tile<RM>;
+  constexpr int BM = S::BM;
+  extern __shared__ __align__(16) float sm[];
+  const int tid = threadIdx.x, grp = tid / kGroup, lt = tid % kGroup, tx = lt & 15, ty = lt >> 4;       // rows ty + 8 i, outputs tx + 16 j
+  const int n0 = (int)blockIdx.x * TN, m0 = (int)blockIdx.y * BM, splits = (int)gridDim.z, z = (int)blockIdx.z;
+  const int k0 = z * k_part, k1 = min(p.k, k0 + k_part), steps = k1 > k0 ? (k1 - k0 + TK - 1) / TK : 0;
+  pdl_wait();
+  pdl_launch_dependents();
+  // a step's operands: rows of x, then rows of W, four k-elements a thread and chunk
+  auto fetch = [&](int step) {
+    constexpr int ALL = (BM + TN) * (TK / 4), N = (ALL + kTileThreads - 1) / kTileThreads;
+    float* dst = sm + (step % kTileStages) * S::STAGE;
+    float4 v[sizeof(T) == 4 && WIDE ? 1 : N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + i * kTileThreads, r = e / (TK / 4), kk = (e % (TK / 4)) * 4, k = k0 + step * TK + kk;
+      if (ALL % kTileThreads != 0 && e >= ALL) break;
+      const T* row = r < BM ? reinterpret_cast<const T*>(p.x) + (long long)min(m0 + r, p.rows - 1) * p.x_row
+                            : reinterpret_cast<const T*>(p.w) + (long long)min(n0 + r - BM, p.n - 1) * p.w_row;
+      if constexpr (sizeof(T) == 4 && WIDE) {
+        cp_async_16(smem_u32(dst + r * kPitch + kk), k < k1 ? row + k : row, k < k1 ? 16u : 0u);      // (k, k1: multiples of 4)
+      } else {
+        float2 h[2];
+        load_pairs<T, 4, WIDE>(row, k, k1, h);
+        v[i] = make_float4(h[0].x, h[0].y, h[1].x, h[1].y);
+      }
+    }
+    if constexpr (!(sizeof(T) == 4 && WIDE)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int e = tid + i * kTileThreads, r = e / (TK / 4), kk = (e % (TK / 4)) * 4;
+        if (ALL % kTileThreads != 0 && e >= ALL) break;
+        *reinterpret_cast<float4*>(dst + r * kPitch + kk) = v[i];
+      }
+    }
+  };
+  float2 acc[RM][4];                             // sums of even and of odd k-elements
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int s = 0; s < kTileStages - 1; ++s) {
+    if (s < steps) fetch(s);
+    cp_async_commit();
+  }
+  for (int s = 0; s < steps; ++s) {
+    cp_async_wait<kTileStages - 2>();
+    __syncthreads();
+    if (s + kTileStages - 1 < steps) fetch(s + kTileStages - 1);
+    cp_async_commit();
+    const float* xs = sm + (s % kTileStages) * S::STAGE;
+    const float* ws = xs + BM * kPitch;
+#pragma unroll
+    for (int kk = grp * 4; kk < TK; kk += 8) {
+      float4 a[RM], b[4];
+#pragma unroll
+      for (int i = 0; i < RM; ++i) a[i] = *reinterpret_cast<const float4*>(xs + (ty + 8 * i) * kPitch + kk);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(ws + (tx + 16 * j) * kPitch + kk);
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), acc[i][j]);
+          acc[i][j] = __ffma2_rn(make_float2(a[i].z, a[i].w), make_float2(b[j].z, b[j].w), acc[i][j]);
+        }
+    }
+  }
+  cp_async_wait<0>();
+  __syncthreads();
+  // ---- the groups' sums over the ring, then the cluster's
+  float* mine = sm + grp * S::SUMS;
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine[(ty + 8 * i) * (TN + 4) + tx + 16 * j] = acc[i][j].x + acc[i][j].y;
+  __syncthreads();
+  if (splits > 1) {
+    for (int e = tid; e < BM * (TN / 4); e += kTileThreads) {
+      float* at = sm + (e / (TN / 4)) * (TN + 4) + (e % (TN / 4)) * 4;
+      const float4 other = *reinterpret_cast<const float4*>(at + S::SUMS);
+      float4 own = *reinterpret_cast<float4*>(at);
+      own.x += other.x; own.y += other.y; own.z += other.z; own.w += other.w;
+      *reinterpret_cast<float4*>(at) = own;
+    }
+    cluster_sync_all();
+  }
+  const int rows_own = (BM + splits - 1) / splits, r_end = min(BM, (z + 1) * rows_own);
+  for (int r = z * rows_own + tid / (TN / 4); r < r_end; r += kTileThreads / (TN / 4)) {
+    const int m = m0 + r, c = (tid % (TN / 4)) * 4;
+    const uint32_t at = smem_u32(sm + r * (TN + 4) + c);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (splits > 1) {
+      for (int s = 0; s < splits; ++s) {
+        const uint32_t from = map_to_cta(at, (uint32_t)s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(ld_cluster_u32(from + 4 * i));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = sm[r * (TN + 4) + c + i] + sm[S::SUMS + r * (TN + 4) + c + i];
+    }
+    if (m < p.rows) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (p.bias && n0 + c + i < p.n) v[i] += p.bias[n0 + c + i];
+      activate(v, p.act);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = n0 + c + i;
+        if (n < p.n) {
+          if (p.resid) v[i] += (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n];
+          reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)v[i];
+        }
+      }
+    }
+  }
+  if (splits > 1) cluster_sync_all();            // nobody leaves while its sums are read
+}
+
+// Splits of the k-elements: enough CTAs for two an SM, each with at least 128 of them.
+int pick_splits(long long tiles, int k) {
+  int s = 1;
+  while (s < 8 && tiles * s * 2 <= 2 * kSms && k >= s * 2 * 128) s *= 2;
+  return s;
+}
+template <typename T, int RM, bool WIDE>
+cudaError_t launch_tile_as(const LinearParams& p, cudaStream_t st) {
+  static std::atomic<unsigned long long> attr{0};
+  auto kern = linear_tile_kernel<T, RM, WIDE>;
+  if (cudaError_t e = ensure_dyn_smem(kern, Tile<RM>::BYTES, attr); e != cudaSuccess) return e;
+  const unsigned nt = (unsigned)((p.n + TN - 1) / TN), mt = (unsigned)((p.rows + Tile<RM>::BM - 1) / Tile<RM>::BM);
+  const int splits = pick_splits((long long)nt * mt, p.k), part = ((p.k + splits - 1) / splits + TK - 1) / TK * TK;
+  // (rows over y, which stops at 65535: more of them in several launches)
+  for (unsigned m = 0; m < mt; m += 65535) {
+    LinearParams q = p;
+    const long long r0 = (long long)m * Tile<RM>::BM;
+    q.x = reinterpret_cast<const T*>(p.x) + r0 * p.x_row;
+    q.y = reinterpret_cast<T*>(p.y) + r0 * p.y_row;
+    if (p.resid) q.resid = reinterpret_cast<const T*>(p.resid) + r0 * p.resid_row;
+    q.rows = (int)(p.rows - r0);
+    const unsigned ny = mt - m < 65535 ? mt - m : 65535;
+    if (ny == 65535 && mt - m > 65535) q.rows = 65535 * Tile<RM>::BM;
+    if (cudaError_t e = launch_pdl(kern, dim3(nt, ny, splits), dim3(kTileThreads), Tile<RM>::BYTES, st, splits, q, part); e != cudaSuccess)
+      return e;
+  }
+  return cudaSuccess;
+}
+template <typename T, bool WIDE>
+cudaError_t launch_tile_by(const LinearParams& p, cudaStream_t st) {
+  if (p.rows <= 8) return launch_tile_as<T, 1, WIDE>(p, st);
+  if (p.rows <= 16) return launch_tile_as<T, 2, WIDE>(p, st);
+  if (p.rows <= 32 || (long long)((p.rows + 63) / 64) * ((p.n + TN - 1) / TN) < kSms) return launch_tile_as<T, 4, WIDE>(p, st);
+  return launch_tile_as<T, 8, WIDE>(p, st);
+}
+
 template <typename T>
-cudaError_t launch_rows(const LinearParams& p, cudaStream_t st) {
-  const uintptr_t mask = 4 * sizeof(T) - 1;
-  const bool wide = p.k % 4 == 0 && p.x_row % 4 == 0 && p.w_row % 4 == 0 && (reinterpret_cast<uintptr_t>(p.x) & mask) == 0 &&
-                    (reinterpret_cast<uintptr_t>(p.w) & mask) == 0;
-  if (p.rows == 1) return launch_rows_as<T, 1>(p, wide, st);
-  if (p.rows == 2) return launch_rows_as<T, 2>(p, wide, st);
-  if (p.rows <= 4) return launch_rows_as<T, 4>(p, wide, st);
-  if (p.rows <= 8) return launch_rows_as<T, 8>(p, wide, st);
-  return launch_rows_as<T, 16>(p, wide, st);
+cudaError_t launch_simt(const LinearParams& p, cudaStream_t st) {
+  // rows that 16-byte (rows kernel) or four-element accesses can follow
+  auto wide = [&](int elements) {
+    const uintptr_t mask = elements * sizeof(T) - 1;
+    return (p.rows == 1 || p.x_row % elements == 0) && (p.n == 1 || p.w_row % elements == 0) && (reinterpret_cast<uintptr_t>(p.x) & mask) == 0 &&
+           (reinterpret_cast<uintptr_t>(p.w) & mask) == 0;
+  };
+  constexpr int VE = 16 / sizeof(T);
+  if (p.rows <= 4) return wide(VE) ? launch_rows_by<T, VE, true>(p, st) : launch_rows_by<T, 4, false>(p, st);
+  return wide(4) && p.k % 4 == 0 ? launch_tile_by<T, true>(p, st) : launch_tile_by<T, false>(p, st);
 }
 }  // namespace
 
 cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, cudaStream_t st) {
-  return bf16 ? launch_rows<__nv_bfloat16>(p, st) : launch_rows<float>(p, st);
+  return bf16 ? launch_simt<__nv_bfloat16>(p, st) : launch_simt<float>(p, st);
 }
 
 }  // namespace dare
 
 using namespace dare;
+
+namespace {
+constexpr int kRowsOnCudaCores = 4;        // bf16
+}
 
 extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* x, const void* w, const float* bias, const void* resid,
                                      void* y, int32_t* status, void* cuda_stream) {
@@ -168,17 +360,16 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   cudaError_t e;
   if (c->dtype == DARE_BF16) {
     const bool tc = !low(x, 15u) && !low(w, 15u) && strides(c->rows, c->x_row, 8) && strides(c->out_features, c->w_row, 8);
-    e = tc ? launch_linear_tc(p, st) : launch_linear_simt(p, true, st);
+    e = tc && p.rows > kRowsOnCudaCores ? launch_linear_tc(p, st) : launch_linear_simt(p, true, st);
   } else {
     const bool aligned = !low(x, 15u) && !low(w, 15u) && c->in_features % 4 == 0 && strides(c->rows, c->x_row, 4) &&
                          strides(c->out_features, c->w_row, 4);
-    // CUDA cores: 80 cycles a step of 16 rows x 4 outputs x 128 elements on an SM; tensor cores: a tile of 128 rows x 64 outputs takes 4.5 us
-    // and 1.1 us a block of 64 elements.
-    const float here = (float)((c->rows + 15) / 16) * (float)((c->out_features + 3) / 4) * (float)((c->in_features + 127) / 128) *
-                           (80.f / 1900.f / (float)kSms) + 4.f;
+    // On the tensor cores a tile of 128 rows x 64 outputs takes 4.5 us and 1.1 us a block of 64 k-elements; on the CUDA cores an SM
+    // does about 70 multiply-adds a cycle and a launch takes 6 us at least.
     const int64_t tiles = (c->rows + 127) / 128 * ((c->out_features + 63) / 64);
     const float there = (float)((tiles + kSms - 1) / kSms) * (4.5f + 1.1f * (float)((c->in_features + 63) / 64)) + 2.f;
-    e = aligned && there < here ? launch_linear_f32(p, st) : launch_linear_simt(p, false, st);
+    const float here = 6.f + (float)((c->rows + 31) / 32 * 32) * (float)c->out_features * (float)c->in_features / (70.f * 1900.f * (float)kSms);
+    e = aligned && p.rows > 4 && there < here ? launch_linear_f32(p, st) : launch_linear_simt(p, false, st);
   }
   if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }
   return DARE_OK;

@@ -3,9 +3,10 @@
 // finishing pass of a tile running beside the next one's main loop.  The width is not fixed: it is what the launch rule below
 // finds cheapest, a multiple of 16 up to 256.  With few rows the launch is a stream of W and the width is the outputs over the SMs,
 // so that every SM pulls its share at the same time and no reduction has to be split; only the rows there are come into shared
-// memory then (the MMA's other rows read whatever follows, and nobody reads their results), which leaves up to 24 stages of W on
+// memory then (the MMA's other rows read whatever follows, and nobody reads their results), which leaves up to 12 stages of W on
 // their way.
-//   warp 0     TMA producer: rows of x and of W, 64 k-elements a stage; rows, columns and k-elements past the end are zeros
+//   warp 0     TMA producer: rows of x and of W, 128 k-elements a stage in two boxes of 64 columns each (256 bytes of a row of W come
+//              from one place of the HBM at a time); rows, columns and k-elements past the end are zeros
 //   warp 1     MMA issuer (of a pair: the even CTA's), two accumulators of up to 256 columns of tensor memory in turn
 //   warps 2-9  finishing pass, two warps a lane quarter, thread <-> row, 32 columns at a time: bias, activation, residual, store
 #include "linear.h"
@@ -17,9 +18,10 @@ namespace dare {
 using namespace ptx;
 
 namespace {
-constexpr int BM = 128, BK = 64, kFinish = 8, kThreads = (2 + kFinish) * 32;
-constexpr int kRing = 192 * 1024, kMaxStages = 24;
-constexpr int BAR_OFFSET = kRing + BM * BK * 2;            // (an MMA reads 128 rows from where a stage's rows of x begin)
+constexpr int BM = 128, BK = 128, kFinish = 8, kThreads = (2 + kFinish) * 32;
+constexpr int kRing = 192 * 1024, kMaxStages = 12;
+constexpr int HALF_X = BM * 128;                           // 128 rows of 64 k-elements, what an MMA reads as its rows of x ...
+constexpr int BAR_OFFSET = kRing + HALF_X;                 // ... from where a stage's begin, however few it has
 constexpr int SMEM_TOTAL = BAR_OFFSET + 512 + 1024;
 static_assert(SMEM_TOTAL <= 227 * 1024 && (2 * kMaxStages + 4) * 8 + 4 <= 512, "shared memory of one CTA");
 constexpr int kGroupBytes = 24 << 20;                      // column tiles are walked in groups of this much of W, as in gemm_persist.cu
@@ -45,8 +47,9 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int pr = PAIR ? (int)cluster_ctarank() : 0;
   const int walker = PAIR ? (int)blockIdx.x / 2 : (int)blockIdx.x, n_walkers = PAIR ? (int)gridDim.x / 2 : (int)gridDim.x;
-  const int w_rows = PAIR ? t.width / 2 : t.width, x_bytes = t.x_rows * BK * 2, stage_bytes = x_bytes + w_rows * BK * 2;
-  const int stages = min(kMaxStages, kRing / stage_bytes), KB = (p.k + BK - 1) / BK, total = t.n_tiles * t.m_units;
+  const int w_rows = PAIR ? t.width / 2 : t.width, x_bytes = t.x_rows * BK * 2, w_bytes = w_rows * BK * 2, stage_bytes = x_bytes + w_bytes;
+  const int stages = min(kMaxStages, kRing / stage_bytes), KB = (p.k + BK - 1) / BK, k16 = (p.k + 15) / 16 * 16;
+  const int total = t.n_tiles * t.m_units;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
@@ -95,15 +98,20 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         mbar_wait(&empty_bar[s], ((it / stages) & 1) ^ 1, p.status);
         if (elect_one()) {
           uint8_t* dst = smem + s * stage_bytes;
-          if (PAIR) {                 // the bytes of both CTAs are counted on the even one's barrier
-            const uint32_t fb = map_to_cta(smem_u32(&full_bar[s]), 0);
-            if (pr == 0) mbar_arrive_expect_tx(&full_bar[s], 2u * stage_bytes);
-            tma_load_2d_pair(dst, &tm_x, kb * BK, m0, fb);
-            tma_load_2d_pair(dst + x_bytes, &tm_w, kb * BK, n0 + pr * w_rows, fb);
-          } else {
-            mbar_arrive_expect_tx(&full_bar[s], (uint32_t)stage_bytes);
-            tma_load_2d(dst, &tm_x, kb * BK, m0, &full_bar[s]);
-            tma_load_2d(dst + x_bytes, &tm_w, kb * BK, n0, &full_bar[s]);
+          const uint32_t fb = PAIR ? map_to_cta(smem_u32(&full_bar[s]), 0) : 0;
+          // (PAIR: the bytes of both CTAs are counted on the even one's barrier)
+          if (!PAIR) mbar_arrive_expect_tx(&full_bar[s], (uint32_t)stage_bytes);
+          else if (pr == 0) mbar_arrive_expect_tx(&full_bar[s], 2u * stage_bytes);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int k0 = kb * BK + h * 64;
+            if (PAIR) {
+              tma_load_2d_pair(dst + h * (x_bytes / 2), &tm_x, k0, m0, fb);
+              tma_load_2d_pair(dst + x_bytes + h * (w_bytes / 2), &tm_w, k0, n0 + pr * w_rows, fb);
+            } else {
+              tma_load_2d(dst + h * (x_bytes / 2), &tm_x, k0, m0, &full_bar[s]);
+              tma_load_2d(dst + x_bytes + h * (w_bytes / 2), &tm_w, k0, n0, &full_bar[s]);
+            }
           }
         }
         __syncwarp();
@@ -124,10 +132,13 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
           if (elect_one()) {
             const uint32_t at = smem_u32(smem + s * stage_bytes);
             const uint64_t a = smem_desc_k_sw128(at), b = smem_desc_k_sw128(at + x_bytes);
+            const int steps = min(BK, k16 - kb * BK) / 16;          // (the last block's k-elements past the end are not there)
 #pragma unroll
             for (int k = 0; k < BK / 16; ++k) {
-              if (PAIR) umma2_ss(d_tmem, a + 2 * k, b + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
-              else umma_ss(d_tmem, a + 2 * k, b + 2 * k, idesc, (kb | k) != 0 ? 1u : 0u);
+              if (k >= steps) break;
+              const uint64_t ak = a + (k >> 2) * (uint32_t)(x_bytes >> 5) + 2 * (k & 3), bk = b + (k >> 2) * (uint32_t)(w_bytes >> 5) + 2 * (k & 3);
+              if (PAIR) umma2_ss(d_tmem, ak, bk, idesc, (kb | k) != 0 ? 1u : 0u);
+              else umma_ss(d_tmem, ak, bk, idesc, (kb | k) != 0 ? 1u : 0u);
             }
             if (PAIR) {
               umma2_commit(map_to_cta(smem_u32(&empty_bar[s]), 0));
@@ -159,15 +170,14 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
       const bool warp_has_rows = m0 + q * 32 < p.rows;
       __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (long long)row * p.y_row + n0;
       const __nv_bfloat16* resid = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + (long long)row * p.resid_row + n0 : nullptr;
-      if (warp_has_rows) {
+      if (warp_has_rows && t.wide_y) {
 #pragma unroll 1
         for (int c = sub * 32; c < cols; c += 64) {
           const bool full = c + 32 <= cols;
           float v[32];
           tmem_ld_32x32_nowait(t_lane + c, v);
           uint4 rs[4];
-          const bool wide = full && t.wide_y;
-          if (resid && wide && row < p.rows) {
+          if (resid && full && row < p.rows) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) rs[i] = *reinterpret_cast<const uint4*>(resid + c + 8 * i);
           }
@@ -188,7 +198,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
           }
           activate(v, p.act);
           if (row < p.rows) {
-            if (wide) {
+            if (full) {
               if (resid) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -215,6 +225,42 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
           }
           __syncwarp();
         }
+      } else if (warp_has_rows) {
+        // Rows of y or resid that are not on the 16-byte grid: 16 columns at a time through 2 KB of shared memory (the rows that the
+        // last stage's MMA reads past its own; units of 16 bytes swizzled by row), from where half a warp takes a row: 2-byte
+        // stores of 32 rows at a time took as long as the main loop (3080 x 6400 x 1899: 111 us).
+        float* stg = reinterpret_cast<float*>(smem + kRing) + (warp - 2) * (32 * 16);
+        const int lr = lane >> 4, lc = lane & 15;
+#pragma unroll 1
+        for (int c = sub * 16; c < cols; c += 32) {
+          float v[16];
+          tmem_ld_32x16_nowait(t_lane + c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4*>(stg + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          __syncwarp();
+          const bool there = c + lc < cols;
+          const float bias = p.bias && there ? __ldg(p.bias + n0 + c + lc) : 0.f;
+          const int rows = min(32, p.rows - (m0 + q * 32));
+          float o[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = 2 * i + lr;
+            o[i] = stg[r * 16 + ((((lc >> 2) ^ ((r >> 1) & 3)) << 2) | (lc & 3))] + bias;
+          }
+          activate(o, p.act);
+          const long long row0 = m0 + q * 32 + lr;
+          const __nv_bfloat16* rp = reinterpret_cast<const __nv_bfloat16*>(p.resid) + (p.resid ? row0 * p.resid_row + n0 + c + lc : 0);
+          __nv_bfloat16* yp = reinterpret_cast<__nv_bfloat16*>(p.y) + row0 * p.y_row + n0 + c + lc;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (there && 2 * i + lr < rows) {
+              if (p.resid) o[i] += __bfloat162float(rp[2 * i * p.resid_row]);
+              yp[2 * i * p.y_row] = __float2bfloat16_rn(o[i]);
+            }
+          __syncwarp();
+        }
       }
       tc_fence_before();
       __syncwarp();
@@ -232,7 +278,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
   }
 }
 
-// Tile width and form: waves of tiles times what a 64-element k-block takes an SM (the tensor pipe's cycles, or the operand bytes
+// Tile width and form: waves of tiles times what a k-block takes an SM (the tensor pipe's cycles, or the operand bytes
 // at 64 a cycle), plus the finishing pass of the last tile.
 struct Form { int pair, width; };
 Form pick_form(int rows, int n, int k) {
@@ -243,8 +289,8 @@ Form pick_form(int rows, int n, int k) {
     for (int width = pair ? 32 : 16; width <= 256; width += pair ? 32 : 16) {
       const int units = (n + width - 1) / width * (pair ? (m_tiles + 1) / 2 : m_tiles), slots = pair ? kSms / 2 : kSms;
       const float waves = (float)((units + slots - 1) / slots);
-      const float mma = 4.f * fmaxf(48.f, 129.f * (float)width / 256.f);
-      const float feed = (float)(x_rows * 128 + (pair ? width / 2 : width) * 128) / 64.f;
+      const float mma = 8.f * fmaxf(48.f, 129.f * (float)width / 256.f);
+      const float feed = (float)(x_rows + (pair ? width / 2 : width)) * (float)(BK * 2) / 64.f;
       const float cycles = waves * (float)KB * fmaxf(mma, feed) + 6.f * (float)width;
       if (cycles < least) { least = cycles; best = Form{pair, width}; }
     }

@@ -52,37 +52,52 @@ __global__ void __launch_bounds__(128) rope_freq_table_kernel(const Frequencies 
 // and behind them units of VEC elements that are copied (none in place).
 constexpr int kHeads = 4, kThreads = 256;
 
+// VEC elements, kept as they were read until they are used: a unit's heads are all on their way while the position and then the
+// table's row are.
 template <typename T, int VEC>
 struct Chunk {
-  float v[VEC];
+  static constexpr bool kWide = VEC * sizeof(T) == 16;
+  union {
+    uint4 vec;
+    T el[VEC];
+  };
+  __device__ __forceinline__ Chunk() {}
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (VEC * sizeof(T) == 16) {
-      const uint4 raw = *reinterpret_cast<const uint4*>(p);
-      if constexpr (sizeof(T) == 4) {
-        const float* f = reinterpret_cast<const float*>(&raw);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = f[i];
-      } else {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
-#pragma unroll
-        for (int i = 0; i < VEC / 2; ++i) {
-          const float2 f = __bfloat1622float2(h[i]);
-          v[2 * i] = f.x;
-          v[2 * i + 1] = f.y;
-        }
-      }
+    if constexpr (kWide) {
+      vec = *reinterpret_cast<const uint4*>(p);
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = (float)p[i];
+      for (int i = 0; i < VEC; ++i) el[i] = p[i];
     }
   }
   __device__ __forceinline__ void store(T* p) const {
-    if constexpr (VEC * sizeof(T) == 16) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      else *reinterpret_cast<uint4*>(p) = pack8_bf16(v);
+    if constexpr (kWide) {
+      *reinterpret_cast<uint4*>(p) = vec;
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) p[i] = (T)v[i];
+      for (int i = 0; i < VEC; ++i) p[i] = el[i];
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[VEC]) const {
+    if constexpr (kWide && sizeof(T) == 2) {
+      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&vec);
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) {
+        const float2 f = __bfloat1622float2(h[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = (float)el[i];
+    }
+  }
+  __device__ __forceinline__ void put(const float (&v)[VEC]) {
+    if constexpr (kWide && sizeof(T) == 2) {
+      vec = pack8_bf16(v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) el[i] = (T)v[i];
     }
   }
 };
@@ -100,7 +115,7 @@ struct RopeParams {
 };
 
 template <typename T, int VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const int per_token = p.units * p.chunks;
@@ -109,85 +124,71 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
     const int tl = w / per_token, rest = w - tl * per_token, chunk = rest / p.units, u = rest - chunk * p.units;
     const long long t = t0 + tl;
     if (t >= p.tokens) return;
-    const long long pos = p.positions ? (long long)p.positions[t] : p.pos_begin + t;
+    const long long pos = p.positions ? (long long)__ldg(p.positions + t) : p.pos_begin + t;
+    const int h0 = chunk * kHeads, n = min(kHeads, p.heads - h0);
+    const T* x = reinterpret_cast<const T*>(p.x) + t * p.x_token + h0 * p.x_head;
+    T* y = reinterpret_cast<T*>(p.y) + t * p.y_token + h0 * p.y_head;
+    const bool turns = u < p.turn_units;
+    // a unit's elements: e .. and, of a half-split pair, its partners pairs further on
+    const int e = turns ? u * VEC : p.rotary + (u - p.turn_units) * VEC;
+    const bool whole = Chunk<T, VEC>::kWide || e + VEC <= p.head_dim;        // (a copied part may end in one element)
+    Chunk<T, VEC> a[kHeads], b[HALF ? kHeads : 1];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i)
+      if (i < n) {
+        if (whole) a[i].load(x + i * p.x_head + e);
+        else a[i].el[0] = x[i * p.x_head + e];
+        if (HALF && turns) b[HALF ? i : 0].load(x + i * p.x_head + p.pairs + e);
+      }
     if (pos < 0 || pos >= p.table_positions) {
       flag_device_check(p.status);
       continue;
     }
-    const int h0 = chunk * kHeads, n = min(kHeads, p.heads - h0);
-    const T* x = reinterpret_cast<const T*>(p.x) + t * p.x_token + h0 * p.x_head;
-    T* y = reinterpret_cast<T*>(p.y) + t * p.y_token + h0 * p.y_head;
-    if (u >= p.turn_units) {                                            // the part of the head that does not turn
-      const int e = p.rotary + (u - p.turn_units) * VEC;
-      Chunk<T, VEC> a[kHeads];
+    if (!turns) {
 #pragma unroll
       for (int i = 0; i < kHeads; ++i)
         if (i < n) {
-          if (VEC * sizeof(T) == 16 || e + VEC <= p.head_dim) a[i].load(x + i * p.x_head + e);
-          else a[i].v[0] = (float)x[i * p.x_head + e];
-        }
-#pragma unroll
-      for (int i = 0; i < kHeads; ++i)
-        if (i < n) {
-          if (VEC * sizeof(T) == 16 || e + VEC <= p.head_dim) a[i].store(y + i * p.y_head + e);
-          else y[i * p.y_head + e] = (T)a[i].v[0];
+          if (whole) a[i].store(y + i * p.y_head + e);
+          else y[i * p.y_head + e] = a[i].el[0];
         }
       continue;
     }
-    constexpr int PAIRS = HALF ? VEC : VEC / 2;                          // pairs of a unit
+    constexpr int PAIRS = HALF ? VEC : VEC / 2;                              // pairs of a unit
     const float2* tab = p.table + pos * p.pairs + u * PAIRS;
     const float sign = p.transpose ? -1.f : 1.f;
-    if constexpr (HALF) {
-      Chunk<T, VEC> a[kHeads], b[kHeads];
-      const int e = u * VEC;
+    float2 cs[PAIRS];
 #pragma unroll
-      for (int i = 0; i < kHeads; ++i)
-        if (i < n) {
-          a[i].load(x + i * p.x_head + e);
-          b[i].load(x + i * p.x_head + p.pairs + e);
-        }
-      float2 cs[PAIRS];
+    for (int k = 0; k < PAIRS; ++k) {
+      cs[k] = __ldg(tab + k);
+      cs[k].y *= sign;
+    }
 #pragma unroll
-      for (int k = 0; k < PAIRS; ++k) {
-        cs[k] = tab[k];
-        cs[k].y *= sign;
-      }
-#pragma unroll
-      for (int i = 0; i < kHeads; ++i)
-        if (i < n) {
+    for (int i = 0; i < kHeads; ++i)
+      if (i < n) {
+        float va[VEC];
+        a[i].get(va);
+        if constexpr (HALF) {
+          float vb[VEC];
+          b[i].get(vb);
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            const float s = a[i].v[k], r = b[i].v[k];
-            a[i].v[k] = s * cs[k].x - r * cs[k].y;
-            b[i].v[k] = r * cs[k].x + s * cs[k].y;
+            const float s = va[k], r = vb[k];
+            va[k] = s * cs[k].x - r * cs[k].y;
+            vb[k] = r * cs[k].x + s * cs[k].y;
           }
-          a[i].store(y + i * p.y_head + e);
+          b[i].put(vb);
           b[i].store(y + i * p.y_head + p.pairs + e);
-        }
-    } else {
-      Chunk<T, VEC> a[kHeads];
-      const int e = u * VEC;
-#pragma unroll
-      for (int i = 0; i < kHeads; ++i)
-        if (i < n) a[i].load(x + i * p.x_head + e);
-      float2 cs[PAIRS];
-#pragma unroll
-      for (int k = 0; k < PAIRS; ++k) {
-        cs[k] = tab[k];
-        cs[k].y *= sign;
-      }
-#pragma unroll
-      for (int i = 0; i < kHeads; ++i)
-        if (i < n) {
+        } else {
 #pragma unroll
           for (int k = 0; k < PAIRS; ++k) {
-            const float s = a[i].v[2 * k], r = a[i].v[2 * k + 1];
-            a[i].v[2 * k] = s * cs[k].x - r * cs[k].y;
-            a[i].v[2 * k + 1] = r * cs[k].x + s * cs[k].y;
+            const float s = va[2 * k], r = va[2 * k + 1];
+            va[2 * k] = s * cs[k].x - r * cs[k].y;
+            va[2 * k + 1] = r * cs[k].x + s * cs[k].y;
           }
-          a[i].store(y + i * p.y_head + e);
         }
-    }
+        a[i].put(va);
+        a[i].store(y + i * p.y_head + e);
+      }
   }
 }
 

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libdare.so")
@@ -386,141 +387,188 @@ def _current_stream(torch, device) -> int:
 
 # Stand-alone operators on torch tensors: argument marshalling, outputs and workspaces from torch's allocator, the tensors' device
 # and its current stream.  `status`: an int32 CUDA tensor of one element that device-side problems are recorded in, or None.
-class _on_device:
-    """Makes the tensors' device the current one for a call (a no-op where it is)."""
-
-    def __init__(self, torch, device):
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+# A call takes the host as long as several of the kernels behind it, so the wrappers ask each tensor for its shape and strides
+# once, pack the argument block with struct and leave the wording of refusals to the ends that need one.
+_torch = None
 
 
-def _check(cond, what):
-    if not cond:
-        raise ValueError(what)
+def _use_torch():
+    global _torch, _DTYPES, _stream_of, _device_now
+    import torch
+    _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+    _device_now = torch.cuda.current_device
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _stream_of = raw if raw is not None else (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _torch = torch
+    return torch
 
 
-def _dtype_of(torch, x):
-    _check(x.dtype in (torch.bfloat16, torch.float32), f"bf16 or float32 expected, not {x.dtype}")
-    return BF16 if x.dtype == torch.bfloat16 else F32
+def _same_device(index, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            return False
+    return index >= 0
 
 
-def _same_device(x, *others):
-    _check(x.is_cuda, "CUDA tensors expected")
-    for t in others:
-        _check(t is None or t.device == x.device, "tensors on different devices")
-
-
-def _ptr(t):
-    return t.data_ptr() if t is not None else None
+def _call(fn, name, index, *args):
+    """fn(*args, stream) with the tensors' device current."""
+    if _device_now() == index:
+        st = fn(*args, _stream_of(index))
+    else:
+        with _torch.cuda.device(index):
+            st = fn(*args, _stream_of(index))
+    if st != OK:
+        raise DareError(st, name)
 
 
 def rope_table(positions, rotary_dim, theta, scaling=ROPE_SCALE["none"], factor=1.0, trained=0, low=1.0, high=32.0,
                magnitude=1.0, device="cuda", out=None):
     """-> float32 [positions, rotary_dim / 2, 2]: cosines and sines of dare_rope_table, for `rope`."""
-    import torch
+    torch = _torch or _use_torch()
+    shape = (positions, rotary_dim // 2, 2)
     if out is None:
-        out = torch.empty((positions, rotary_dim // 2, 2), dtype=torch.float32, device=device)
-    _check(out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.shape == (positions, rotary_dim // 2, 2),
-           "out: contiguous float32 CUDA tensor [positions, rotary_dim / 2, 2] expected")
+        out = torch.empty(shape, dtype=torch.float32, device=device)
+    index = out.get_device()
+    if index < 0 or out.dtype != torch.float32 or out.shape != shape or not out.is_contiguous():
+        raise ValueError("out: contiguous float32 CUDA tensor [positions, rotary_dim / 2, 2] expected")
     cfg = RopeConfig(C.sizeof(RopeConfig), rotary_dim, theta, scaling, trained, factor, low, high, magnitude)
-    with _on_device(torch, out.device):
-        st = dare_rope_table(cfg, out.data_ptr(), positions, _current_stream(torch, out.device))
-    if st != OK:
-        raise DareError(st, "dare_rope_table")
+    _call(_lib.dare_rope_table, "dare_rope_table", index, C.byref(cfg), out.data_ptr(), positions)
     return out
+
+
+_ROPE_APPLY = struct.Struct("=Iiqiiiiii5q")           # RopeApply
 
 
 def rope(x, table, positions=None, layout=ROPE_LAYOUT["half"], transpose=False, pos_begin=0, out=None, status=None):
     """x [tokens, heads, head_dim] (any token and head strides) with its heads turned by the table's rows of `positions` (int32
     [tokens]; None: pos_begin, pos_begin + 1, ...).  The table's width gives the part of the head that turns.  out may be x."""
-    import torch
-    dt = _dtype_of(torch, x)
-    _same_device(x, table, positions, out, status)
-    _check(x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1), "x: [tokens, heads, head_dim] with the head's elements side by side")
-    _check(table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous(),
-           "table: contiguous float32 [positions, rotary_dim / 2, 2] expected")
-    _check(positions is None or (positions.dtype == torch.int32 and positions.shape == x.shape[:1] and positions.is_contiguous()),
-           "positions: contiguous int32 [tokens] expected")
+    torch = _torch or _use_torch()
+    dt, index = _DTYPES.get(x.dtype), x.get_device()
+    if dt is None or x.dim() != 3 or table.dtype != torch.float32 or table.dim() != 3 or not _same_device(index, table, positions, out, status):
+        raise ValueError("x: bf16 or float32 CUDA tensor [tokens, heads, head_dim], table: float32 [positions, rotary_dim / 2, 2] on its "
+                         "device expected")
+    tokens, heads, hd = shape = x.shape
+    xt, xh, xe = x.stride()
+    rows, pairs, two = table.shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check(out.shape == x.shape and out.dtype == x.dtype and (out.stride(2) == 1 or x.shape[2] == 1), "out: as x")
-    cfg = RopeApply(C.sizeof(RopeApply), dt, x.shape[0], x.shape[1], x.shape[2], table.shape[1] * 2, layout, 1 if transpose else 0,
-                    pos_begin, x.stride(0), x.stride(1), out.stride(0), out.stride(1), table.shape[0])
-    with _on_device(torch, x.device):
-        st = dare_rope(cfg, x.data_ptr(), _ptr(positions), table.data_ptr(), out.data_ptr(), _ptr(status),
-                       _current_stream(torch, x.device))
-    if st != OK:
-        raise DareError(st, "dare_rope")
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        yt, yh, ye = heads * hd, hd, 1
+    else:
+        yt, yh, ye = out.stride()
+        if out.shape != shape or out.dtype != x.dtype:
+            raise ValueError("out: as x")
+    if hd > 1 and (xe != 1 or ye != 1):
+        raise ValueError("the elements of a head have to lie side by side")
+    if two != 2 or not table.is_contiguous():
+        raise ValueError("table: contiguous [positions, rotary_dim / 2, 2] expected")
+    pos = None
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.shape != shape[:1] or not positions.is_contiguous():
+            raise ValueError("positions: contiguous int32 [tokens] expected")
+        pos = positions.data_ptr()
+    cfg = _ROPE_APPLY.pack(_ROPE_APPLY.size, dt, tokens, heads, hd, 2 * pairs, layout, 1 if transpose else 0, pos_begin, xt, xh, yt,
+                           yh, rows)
+    _call(_fast_rope, "dare_rope", index, cfg, x.data_ptr(), pos, table.data_ptr(), out.data_ptr(),
+          None if status is None else status.data_ptr())
     return out
+
+
+_LINEAR = struct.Struct("=Iiqiiii4q")                 # LinearConfig
 
 
 def linear(x, w, bias=None, act=ACT["none"], resid=None, out=None, status=None):
     """act(x w^T + bias) + resid: x [..., in_features], w [out_features, in_features] (as the layer's weights), bias float32
     [out_features], resid [..., out_features].  Rows may be strided; out may be resid."""
-    import torch
-    dt = _dtype_of(torch, x)
-    _same_device(x, w, bias, resid, out, status)
-    _check(w.dim() == 2 and w.dtype == x.dtype and w.shape[1] == x.shape[-1] and (w.stride(1) == 1 or w.shape[1] == 1),
-           "w: [out_features, in_features] of x's type, its rows' elements side by side")
+    torch = _torch or _use_torch()
+    dtype, index = x.dtype, x.get_device()
+    dt = _DTYPES.get(dtype)
+    if dt is None or w.dtype != dtype or w.dim() != 2 or not _same_device(index, w, bias, resid, out, status):
+        raise ValueError("x: bf16 or float32 CUDA tensor, w: [out_features, in_features] of its type and device expected")
     n, k = w.shape
-    _check(bias is None or (bias.dtype == torch.float32 and bias.shape == (n,) and bias.is_contiguous()),
-           "bias: contiguous float32 [out_features] expected")
-    x2 = x if x.dim() == 2 else x.reshape(-1, k)
-    _check(x2.stride(1) == 1 or k == 1, "the elements of a row of x have to lie side by side")
-    shape = x.shape[:-1] + (n,)
+    shape = x.shape
+    if shape[-1] != k:
+        raise ValueError("x and w: in_features differ")
+    flat = len(shape) == 2
+    x2 = x if flat else x.reshape(-1, k)
+    m = x2.shape[0]
+    shape = (m, n) if flat else shape[:-1] + (n,)
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    for t in (resid, out):
-        _check(t is None or (t.shape == shape and t.dtype == x.dtype), "resid, out: [..., out_features] of x's type expected")
-    y2, r2 = (t if t is None or t.dim() == 2 else t.view(-1, n) for t in (out, resid))
-    _check((y2.stride(1) == 1 or n == 1) and (r2 is None or r2.stride(1) == 1 or n == 1),
-           "the elements of a row of resid and out have to lie side by side")
-    cfg = LinearConfig(C.sizeof(LinearConfig), dt, x2.shape[0], k, n, act, 0, x2.stride(0), w.stride(0),
-                       r2.stride(0) if r2 is not None else 0, y2.stride(0))
-    with _on_device(torch, x.device):
-        st = dare_linear(cfg, x2.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(r2), y2.data_ptr(), _ptr(status),
-                         _current_stream(torch, x.device))
-    if st != OK:
-        raise DareError(st, "dare_linear")
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    elif out.shape != shape or out.dtype != dtype:
+        raise ValueError("out: [..., out_features] of x's type expected")
+    y2 = out if flat else out.view(-1, n)
+    r2, rr, re = resid, 0, 1
+    if resid is not None:
+        if resid.shape != shape or resid.dtype != dtype:
+            raise ValueError("resid: [..., out_features] of x's type expected")
+        r2 = resid if flat else resid.view(-1, n)
+        rr, re = r2.stride()
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
+        raise ValueError("bias: contiguous float32 [out_features] expected")
+    (xr, xe), (wr, we), (yr, ye) = x2.stride(), w.stride(), y2.stride()
+    if (k > 1 and (xe != 1 or we != 1)) or (n > 1 and (ye != 1 or re != 1)):
+        raise ValueError("the elements of a row have to lie side by side")
+    cfg = _LINEAR.pack(_LINEAR.size, dt, m, k, n, act, 0, xr, wr, rr, yr)
+    _call(_fast_linear, "dare_linear", index, cfg, x2.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+          None if r2 is None else r2.data_ptr(), y2.data_ptr(), None if status is None else status.data_ptr())
     return out
+
+
+_ATTENTION = struct.Struct("=Iiiiiiif10q")            # AttentionConfig
 
 
 def attention(q, k, v, q_begin, k_begin, k_len=None, causal=False, scale=None, out=None, return_lse=False, status=None):
     """Softmax attention over packed sequences: q [q_rows, n_heads, head_dim], k and v [k_rows, n_kv_heads, head_dim] (any row and
     head strides); q_begin int32 [batch + 1], k_begin int32 [batch + 1] or, with k_len int32 [batch], [batch].  scale: None for
     head_dim^-0.5.  -> out, or (out, lse float32 [q_rows, n_heads])."""
-    import torch
-    dt = _dtype_of(torch, q)
-    _same_device(q, k, v, q_begin, k_begin, k_len, out, status)
-    _check(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.dtype == q.dtype == v.dtype and q.shape[2] == k.shape[2],
-           "q: [rows, heads, head_dim], k and v: [rows, kv heads, head_dim] of one type expected")
-    _check(q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1, "a head's elements have to lie side by side")
+    torch = _torch or _use_torch()
+    dtype, index = q.dtype, q.get_device()
+    dt = _DTYPES.get(dtype)
+    if dt is None or k.dtype != dtype or v.dtype != dtype or not _same_device(index, k, v, q_begin, k_begin, k_len, out, status):
+        raise ValueError("q, k, v: bf16 or float32 CUDA tensors of one type, everything on one device expected")
+    shape = q.shape
+    rows, heads, hd = shape
+    k_rows, kv_heads, k_hd = k.shape
+    if k_hd != hd or v.shape != k.shape:
+        raise ValueError("q: [rows, heads, head_dim], k and v: [rows, kv heads, head_dim] expected")
     batch = q_begin.shape[0] - 1
-    for t, n in ((q_begin, batch + 1), (k_begin, batch if k_len is not None else batch + 1), (k_len, batch)):
-        _check(t is None or (t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and t.shape[0] >= n),
-               "q_begin, k_begin, k_len: contiguous int32 [batch + 1], [batch + 1] (with k_len: [batch]), [batch] expected")
+    i32 = torch.int32
+    if (q_begin.dtype != i32 or k_begin.dtype != i32 or q_begin.dim() != 1 or k_begin.dim() != 1 or not q_begin.is_contiguous() or
+            not k_begin.is_contiguous() or k_begin.shape[0] < (batch + 1 if k_len is None else batch) or
+            (k_len is not None and (k_len.dtype != i32 or k_len.dim() != 1 or k_len.shape[0] < batch or not k_len.is_contiguous()))):
+        raise ValueError("q_begin, k_begin, k_len: contiguous int32 [batch + 1], [batch + 1] (with k_len: [batch]), [batch] expected")
+    qt, qh, qe = q.stride()
+    kt, kh, ke = k.stride()
+    vt, vh, ve = v.stride()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _check(out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1, "out: as q")
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    cfg = AttentionConfig(C.sizeof(AttentionConfig), dt, batch, q.shape[1], k.shape[1], q.shape[2], 1 if causal else 0,
-                          q.shape[2] ** -0.5 if scale is None else scale, q.shape[0], k.shape[0], q.stride(0), q.stride(1),
-                          k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.stride(0), out.stride(1))
-    nbytes = dare_attention_workspace_bytes(cfg)
-    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
-    with _on_device(torch, q.device):
-        st = dare_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_begin.data_ptr(), k_begin.data_ptr(), _ptr(k_len),
-                            out.data_ptr(), _ptr(lse), work.data_ptr(), nbytes, _ptr(status), _current_stream(torch, q.device))
-    if st != OK:
-        raise DareError(st, "dare_attention")
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        ot, oh, oe = heads * hd, hd, 1
+    else:
+        ot, oh, oe = out.stride()
+        if out.shape != shape or out.dtype != dtype:
+            raise ValueError("out: as q")
+    if qe != 1 or ke != 1 or ve != 1 or oe != 1:
+        raise ValueError("the elements of a head have to lie side by side")
+    cfg = _ATTENTION.pack(_ATTENTION.size, dt, batch, heads, kv_heads, hd, 1 if causal else 0, hd ** -0.5 if scale is None else scale, rows,
+                          k_rows, qt, qh, kt, kh, vt, vh, ot, oh)
+    nbytes = _fast_attention_bytes(cfg)
+    work = torch.empty(nbytes or 16, dtype=torch.uint8, device=q.device)
+    lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    _call(_fast_attention, "dare_attention", index, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_begin.data_ptr(),
+          k_begin.data_ptr(), None if k_len is None else k_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+          work.data_ptr(), nbytes, None if status is None else status.data_ptr())
     return (out, lse) if return_lse else out
+
+
+def _packed_entry(name, rest, res=C.c_int):
+    """The entry point with its argument block given as bytes."""
+    return C.CFUNCTYPE(res, C.c_char_p, *rest)((name, _lib))
+
+
+_fast_rope = _packed_entry("dare_rope", [C.c_void_p] * 6)
+_fast_linear = _packed_entry("dare_linear", [C.c_void_p] * 7)
+_fast_attention = _packed_entry("dare_attention", [C.c_void_p] * 9 + [C.c_size_t] + [C.c_void_p] * 2)
+_fast_attention_bytes = _packed_entry("dare_attention_workspace_bytes", [], C.c_size_t)
 
 
 class Layer:
