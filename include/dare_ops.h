@@ -119,8 +119,8 @@ typedef struct {
   int32_t head_dim;     /* 32, 64, 128 or 256 */
   int32_t causal;
   float scale;          /* > 0 */
-  int64_t q_rows;       /* rows of q, out and lse, <= 2^24 */
-  int64_t k_rows;       /* rows of k and v, < 2^31 */
+  int64_t q_rows;       /* rows of q, out and lse, <= 2^24; q_rows * n_heads < 2^31 */
+  int64_t k_rows;       /* rows of k and v, <= 2^30 */
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head; /* strides */
 } dare_attention_config_t;
 

@@ -8,7 +8,6 @@ using namespace dare;
 namespace {
 
 constexpr int kMaxHeads = 1024;
-constexpr int kMinUnitsTc = 2, kMinUnitsSimt = 1;    // units of kUnitKeys keys that a share has at least
 
 bool valid_config(const dare_attention_config_t* c) {
   if (!c || c->struct_size != sizeof(dare_attention_config_t)) return false;
@@ -22,8 +21,8 @@ bool shape_ok(const dare_attention_config_t* c) {
       c->n_heads % c->n_kv_heads != 0)
     return false;
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return false;
-  if (c->q_rows < 0 || c->q_rows > (int64_t)1 << 24 || c->k_rows < 0 || c->k_rows >= (int64_t)1 << 31) return false;
-  if (c->q_rows * c->n_heads > (int64_t)1 << 31) return false;           // (grids and row numbers stay within 31 bits)
+  if (c->q_rows < 0 || c->q_rows > (int64_t)1 << 24 || c->k_rows < 0 || c->k_rows > (int64_t)1 << 30) return false;
+  if (c->q_rows * c->n_heads >= (int64_t)1 << 31) return false;           // (grids and row numbers stay within 31 bits)
   const int64_t s[8] = {c->q_token, c->q_head, c->k_token, c->k_head, c->v_token, c->v_head, c->o_token, c->o_head};
   for (int64_t v : s)
     if (v < 0 || v >= (int64_t)1 << 38) return false;
@@ -74,21 +73,23 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   };
   const bool tc = tc_types(c) && c->k_rows > 0 && !low(q, 15u) && !low(k, 15u) && !low(v, 15u) && !low(out, 15u) && eights(c->q_token) &&
                   eights(c->q_head) && eights(c->o_token) && eights(c->o_head) && tma(c->k_token, c->k_head) && tma(c->v_token, c->v_head);
-  const int rows = tc ? kTcRows : kSimtRows;
+  const int64_t all = c->q_rows * p.group;
+  const int rows = tc ? kTcRows : (all <= (int64_t)kSimtFewRows * c->batch ? kSimtFewRows : kSimtRows);
   p.n_ctas = tc ? kSms : kSimtCtas;
-  p.min_units = tc ? kMinUnitsTc : kMinUnitsSimt;
+  p.group_magic = ((1u << 24) + p.group - 1) / p.group;
+  p.unit_shift = kUnitShift;
+  while ((all / rows + c->batch) * c->n_kv_heads >= ((int64_t)1 << 31) / ((c->k_rows >> p.unit_shift) + 2)) ++p.unit_shift;
   p.part_ml = reinterpret_cast<float2*>(workspace);
   p.part_o = reinterpret_cast<float*>(p.part_ml + part_rows(tc));
 
   cudaError_t e;
   if (tc) {
     // 256 rows a CTA where the sequences have more than one tile's rows on average and that fills the device, shares otherwise.
-    const int64_t all = c->q_rows * p.group;
     const bool tiles = all > (int64_t)kTcRows * c->batch && (all / 256) * c->n_kv_heads >= 3 * kSms / 4;
     e = launch_packed_tc(p, c->head_dim, tiles, st);
     if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);
   } else {
-    e = launch_packed_simt(p, c->head_dim, c->dtype == DARE_BF16, st);
+    e = launch_packed_simt(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
     if (e == cudaSuccess) e = launch_packed_combine(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
   }
   if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }

@@ -10,12 +10,13 @@ using namespace ptx;
 namespace {
 
 // ------------------------------------------------------------------------------------------------ CUDA cores
-// A CTA walks the segments of its share with tiles of 32 rows; two groups of 128 threads take every second block of BKV keys and
-// are merged at the end of a segment.  A thread owns 4 rows: scores of BKV / 16 keys each, then HD / 16 columns of the output each;
+// A CTA walks the segments of its share with tiles of 32 rows (8 where the sequences have no more, as in decoding: a thread then has one
+// row instead of four); two groups of 128 threads take every second block of BKV keys and
+// are merged at the end of a segment.  A thread owns 4 (1) rows: scores of BKV / 16 keys each, then HD / 16 columns of the output each;
 // the 16 lanes of a half-warp share their rows, so the softmax is shuffles and the weights pass through shared memory inside the
 // half-warp.  Two CTAs an SM, so that one multiplies while the other is between two segments.  Everything in fp32.  Bound by the FMA pipe and the shared-memory reads that feed it (8 16-byte reads to 64 FMAs).
-constexpr int BQ = kSimtRows, KG = 2, GROUP = 128, kThreads = KG * GROUP;
-template <int HD>
+constexpr int KG = 2, GROUP = 128, kThreads = KG * GROUP;
+template <int HD, int BQ>
 struct Sm {
   static constexpr int BKV = HD == 256 ? 16 : (HD == 128 ? 32 : 64), JN = BKV / 16;
   static constexpr int KP = HD + 4, PP = BKV + 4;                         // pitches (floats)
@@ -43,13 +44,14 @@ __device__ __forceinline__ float4 load4(const T* src, bool wide) {
   }
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int BQ>
 __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedParams p, const bool wide) {
-  using S = Sm<HD>;
+  using S = Sm<HD, BQ>;
+  constexpr int RI = BQ / 8;                                                // rows of a thread
   constexpr int BKV = S::BKV, JN = S::JN, KP = S::KP, PP = S::PP, VW = S::VW, NC = S::NC;
   extern __shared__ __align__(16) float sm[];
   __shared__ Place pl_sh;
-  __shared__ long long share_sh[2];
+  __shared__ unsigned share_sh[2];
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, grp = tid / GROUP, lt = tid % GROUP, tx = lt & 15, ty = lt >> 4;      // rows ty + 8 i
@@ -62,43 +64,44 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
   const T* vg = reinterpret_cast<const T*>(p.v);
   Line<BQ, true> line(p);                        // (used by warp 0)
   if (tid < 32) {
-    const long long total = line.total(), per = share_units<BQ>(p, total), begin = (long long)blockIdx.x * per;
+    const unsigned total = line.total(), per = share_units(p, total), begin = blockIdx.x * per;
     if (tid == 0) {
       share_sh[0] = begin;
-      share_sh[1] = begin + per < total ? begin + per : total;
+      share_sh[1] = min(begin + per, total);
     }
   }
   __syncthreads();
-  const long long share_begin = share_sh[0], share_end = share_sh[1];
-  for (long long u = share_begin; u < share_end;) {
+  const unsigned share_begin = share_sh[0], share_end = share_sh[1];
+  for (unsigned u = share_begin; u < share_end;) {
     if (tid < 32) {
       Place pl;
       if (line.find(u, &pl) && tid == 0) pl_sh = pl;
     }
     __syncthreads();
     const Place pl = pl_sh;
-    const int row0 = pl.tile * BQ, rows = (int)min((long long)BQ, (long long)pl.s.nq * p.group - row0);
-    const long long pair_end = pl.first + pl.units, end = pair_end < share_end ? pair_end : share_end;
+    const int row0 = pl.tile * BQ, rows = min(BQ, pl.s.nq * p.group - row0);
+    const TileRows tr = tile_rows(p, row0);
+    const unsigned pair_end = pl.first + pl.units, end = min(pair_end, share_end);
     const bool whole = u == pl.first && end == pair_end;
     const int slot = whole ? -1 : 2 * (int)blockIdx.x + (pl.first <= share_begin ? 0 : 1);
-    const int last_seen = keys_seen(p, pl.s, (row0 + rows - 1) / p.group);
-    const int key0 = (int)(u - pl.first) * kUnitKeys, key1 = min(last_seen, (int)min((end - pl.first) * kUnitKeys, 0x7fffffffll));
+    const int last_seen = keys_seen(p, pl.s, row_at(p, tr, 0, rows - 1).query);
+    const int key0 = (int)((u - pl.first) << p.unit_shift), key1 = min(last_seen, (int)((end - pl.first) << p.unit_shift));
     for (int i = tid; i < BQ * (HD / 4); i += kThreads) {
       const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < rows) {
-        const RowAt at = row_at(p, pl, row0 + r);
+        const RowAt at = row_at(p, tr, pl.h, r);
         x = load4(q + (long long)(pl.s.q0 + at.query) * p.q_token + at.head * p.q_head + d, wide);
       }
       *reinterpret_cast<float4*>(qs + r * KP + d) = x;
     }
-    int seen[4];
+    int seen[RI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) seen[i] = keys_seen(p, pl.s, row_at(p, pl, row0 + min(ty + 8 * i, rows - 1)).query);
-    float m[4], l[4];
-    float2 acc[4][NC * VW / 2];
+    for (int i = 0; i < RI; ++i) seen[i] = keys_seen(p, pl.s, row_at(p, tr, 0, min(ty + 8 * i, rows - 1)).query);
+    float m[RI], l[RI];
+    float2 acc[RI][NC * VW / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
 #pragma unroll
@@ -140,20 +143,20 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
     for (int kb = key0 + grp * BKV; kb < key1; kb += KG * BKV) {
       cp_async_wait<1>();                                 // the keys are here
       group_sync();
-      float2 s2[4][JN];                                   // sums over even and over odd elements
+      float2 s2[RI][JN];                                   // sums over even and over odd elements
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RI; ++i)
 #pragma unroll
         for (int j = 0; j < JN; ++j) s2[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
       for (int d = 0; d < HD; d += 4) {
-        float4 a[4], b[JN];
+        float4 a[RI], b[JN];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(qs + (ty + 8 * i) * KP + d);
+        for (int i = 0; i < RI; ++i) a[i] = *reinterpret_cast<const float4*>(qs + (ty + 8 * i) * KP + d);
 #pragma unroll
         for (int j = 0; j < JN; ++j) b[j] = *reinterpret_cast<const float4*>(ks + (tx + 16 * j) * KP + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
           for (int j = 0; j < JN; ++j) {
             s2[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), s2[i][j]);
@@ -163,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
       group_sync();                                       // everybody is through with the keys
       fetch_k(kb + KG * BKV);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < RI; ++i) {
         float top = -INFINITY, s[JN];
 #pragma unroll
         for (int j = 0; j < JN; ++j) {
@@ -189,9 +192,9 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
       group_sync();
 #pragma unroll 2
       for (int j = 0; j < BKV; j += 4) {
-        float4 w[4];
+        float4 w[RI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(ps + (ty + 8 * i) * PP + j);
+        for (int i = 0; i < RI; ++i) w[i] = *reinterpret_cast<const float4*>(ps + (ty + 8 * i) * PP + j);
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj) {
           float2 v[NC * VW / 2];
@@ -202,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
             else v[c] = *reinterpret_cast<const float2*>(src);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < RI; ++i) {
             const float wj = jj == 0 ? w[i].x : (jj == 1 ? w[i].y : (jj == 2 ? w[i].z : w[i].w));
 #pragma unroll
             for (int e = 0; e < NC * VW / 2; ++e) acc[i][e] = __ffma2_rn(make_float2(wj, wj), v[e], acc[i][e]);
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
     // ---- the groups' results over their buffers, merged by everybody
     float* res = ks;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
       const int r = ty + 8 * i;
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
         if (d == 0) p.part_ml[(size_t)slot * BQ + r] = make_float2(top, sum);
       } else {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const RowAt at = row_at(p, pl, row0 + r);
+        const RowAt at = row_at(p, tr, pl.h, r);
         T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d;
         dst[0] = (T)(o.x * inv); dst[1] = (T)(o.y * inv); dst[2] = (T)(o.z * inv); dst[3] = (T)(o.w * inv);
         if (p.lse && d == 0)
@@ -263,122 +266,130 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
   }
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int BQ>
 cudaError_t launch_simt_as(const PackedParams& p, cudaStream_t st) {
   static std::atomic<unsigned long long> attr{0};
-  auto kern = packed_simt_kernel<T, HD>;
-  if (cudaError_t e = ensure_dyn_smem(kern, Sm<HD>::BYTES, attr); e != cudaSuccess) return e;
+  auto kern = packed_simt_kernel<T, HD, BQ>;
+  if (cudaError_t e = ensure_dyn_smem(kern, Sm<HD, BQ>::BYTES, attr); e != cudaSuccess) return e;
   auto whole = [](long long v) { return v % 4 == 0; };
   const uintptr_t mask = 4 * sizeof(T) - 1;
   auto at = [&](const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & mask) == 0; };
   const bool wide = whole(p.q_token) && whole(p.q_head) && whole(p.k_token) && whole(p.k_head) && whole(p.v_token) && whole(p.v_head) &&
                     at(p.q) && at(p.k) && at(p.v);
-  return launch_pdl(kern, dim3((unsigned)p.n_ctas), dim3(kThreads), Sm<HD>::BYTES, st, 1, p, wide);
+  return launch_pdl(kern, dim3((unsigned)p.n_ctas), dim3(kThreads), Sm<HD, BQ>::BYTES, st, 1, p, wide);
 }
 
 // ------------------------------------------------------------------------------------------------ merge
 // o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the shares that hold keys of the row's pair, in the order of the keys (so the
-// result does not depend on which CTA was first).  A CTA has 512 / HD rows of a pair, a thread four columns of one: with one CTA a
-// pair its rows came one after the other, 30 us for tiles of 128 rows.  A pair that lies in one share was written by it.
-constexpr int kCombineThreads = 128;     // (beside a CTA of the kernel before: it waits for that one's end on the SM already)
+// result does not depend on which CTA was first).  blockIdx.x is a cut between two shares; the CTAs of the first cut in a pair merge it,
+// a thread kItems times four columns of a row.  CTAs of two warps: the first 148 fit beside the CTAs of the kernel before, look their
+// cut up there and only wait for its end (CTAs of 256 threads that did so afterwards, each with 8 rows of a pair, were 8 us behind it).
+constexpr int kCombineThreads = 64, kItems = 2;
 template <typename T, int HD, int ROWS>
-__global__ void __launch_bounds__(kCombineThreads) packed_combine_kernel(const PackedParams p) {
-  constexpr int kRows = kCombineThreads / (HD / 4);       // rows of this CTA
+__global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(const PackedParams p) {
   __shared__ Place pl_sh;
-  __shared__ long long per_sh;
+  __shared__ unsigned per_sh;
   __shared__ int more_sh;
   // (the lengths are inputs: complete before the kernel in front let this one start)
   if (threadIdx.x < 32) {
-    // blockIdx.x counts pairs: looked up in the line of pairs, the unit it begins at by the units before it
-    const int lane = threadIdx.x;
     Line<ROWS, true> line(p);
-    const long long per = share_units<ROWS>(p, line.total());
-    line.rewind();
-    long long pairs_before = 0;
-    bool found = false;
-    do {
-      const long long pairs = (long long)line.tiles * p.kv_heads;
-      long long inc = pairs;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, (long long)blockIdx.x < pairs_before + inc);
-      if (hit != 0u) {
-        const int src = __ffs((int)hit) - 1;
-        Place pl;
-        line.place(src, line.base + __shfl_sync(0xffffffffu, line.inc - line.mine, src),
-                   (long long)blockIdx.x - (pairs_before + __shfl_sync(0xffffffffu, inc - pairs, src)), &pl);
-        if (lane == 0) { pl_sh = pl; per_sh = per; }
-        found = true;
-      }
-      pairs_before += __shfl_sync(0xffffffffu, inc, 31);
-    } while (!found && line.next());
-    if (lane == 0) more_sh = found ? 1 : 0;
+    const unsigned per = share_units(p, line.total()), cut = (blockIdx.x + 1) * per;
+    Place pl;
+    const bool found = line.find(cut, &pl) && pl.first < cut && pl.first >= cut - per;
+    if (threadIdx.x == 0) { pl_sh = pl; per_sh = per; more_sh = found ? 1 : 0; }
   }
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
   if (!more_sh) return;
   const Place pl = pl_sh;
-  const long long per = per_sh;
-  const int c0 = (int)(pl.first / per), c1 = (int)((pl.first + pl.units - 1) / per);
-  if (c0 == c1) return;
-  const int row0 = pl.tile * ROWS, rows = (int)min((long long)ROWS, (long long)pl.s.nq * p.group - row0);
+  const unsigned per = per_sh;
+  const int c0 = (int)blockIdx.x, c1 = (int)((pl.first + pl.units - 1) / per);
+  const int row0 = pl.tile * ROWS, rows = min(ROWS, pl.s.nq * p.group - row0);
+  const TileRows tr = tile_rows(p, row0);
   // the first share's part is the last of that CTA (unless the share begins with this pair), the others' their first
-  auto slot_of = [&](int c) { return 2 * c + (c == c0 && pl.first > c0 * per ? 1 : 0); };
-  const int r = (int)blockIdx.y * kRows + (int)threadIdx.x / (HD / 4), d = ((int)threadIdx.x % (HD / 4)) * 4;
-  if (r >= rows) return;
-  float top = -INFINITY;
-#pragma unroll 8
-  for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(p.part_ml + (size_t)slot_of(c) * ROWS + r).x);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
-#pragma unroll 8
-  for (int c = c0; c <= c1; ++c) {
-    const size_t at = (size_t)slot_of(c) * ROWS + r;
-    const float2 ml = __ldcg(p.part_ml + at);
-    const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + d));
-    const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
-    o.x = fmaf(a.x, w, o.x); o.y = fmaf(a.y, w, o.y); o.z = fmaf(a.z, w, o.z); o.w = fmaf(a.w, w, o.w);
-    sum = fmaf(ml.y, w, sum);
+  const int first_slot = 2 * c0 + (pl.first > c0 * per ? 1 : 0);
+  auto slot_of = [&](int c) { return c == c0 ? first_slot : 2 * c; };
+  const int item0 = (int)blockIdx.y * (kCombineThreads * kItems) + (int)threadIdx.x;
+  if (item0 >= rows * (HD / 4)) return;
+  int r[kItems], d[kItems];                      // (past the end: the last item again, not written)
+  float top[kItems], sum[kItems];
+  float4 o[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int item = min(item0 + i * kCombineThreads, rows * (HD / 4) - 1);
+    r[i] = item / (HD / 4);
+    d[i] = (item % (HD / 4)) * 4;
+    top[i] = -INFINITY;
+    sum[i] = 0.f;
+    o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const RowAt at = row_at(p, pl, row0 + r);
-  T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d;
-  dst[0] = (T)(o.x * inv); dst[1] = (T)(o.y * inv); dst[2] = (T)(o.z * inv); dst[3] = (T)(o.w * inv);
-  if (p.lse && d == 0)
-    p.lse[(long long)(pl.s.q0 + at.query) * p.n_heads + at.head] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
+#pragma unroll 2
+  for (int c = c0; c <= c1; ++c)
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) top[i] = fmaxf(top[i], __ldcg(p.part_ml + (size_t)slot_of(c) * ROWS + r[i]).x);
+#pragma unroll 2
+  for (int c = c0; c <= c1; ++c)
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const size_t at = (size_t)slot_of(c) * ROWS + r[i];
+      const float2 ml = __ldcg(p.part_ml + at);
+      const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + d[i]));
+      const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top[i]);
+      o[i].x = fmaf(a.x, w, o[i].x); o[i].y = fmaf(a.y, w, o[i].y); o[i].z = fmaf(a.z, w, o[i].z); o[i].w = fmaf(a.w, w, o[i].w);
+      sum[i] = fmaf(ml.y, w, sum[i]);
+    }
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    if (item0 + i * kCombineThreads >= rows * (HD / 4)) break;
+    const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+    const RowAt at = row_at(p, tr, pl.h, r[i]);
+    T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d[i];
+    dst[0] = (T)(o[i].x * inv); dst[1] = (T)(o[i].y * inv); dst[2] = (T)(o[i].z * inv); dst[3] = (T)(o[i].w * inv);
+    if (p.lse && d[i] == 0)
+      p.lse[(long long)(pl.s.q0 + at.query) * p.n_heads + at.head] = sum[i] == 0.f ? -INFINITY : top[i] * 0.69314718055994531f + logf(sum[i]);
+  }
 }
 template <typename T, int HD, int ROWS>
 cudaError_t launch_combine_as(const PackedParams& p, cudaStream_t st) {
   // (no tile has more rows than there are)
-  constexpr int kRows = kCombineThreads / (HD / 4);
-  const long long all = p.q_rows * p.group, pairs = (all / ROWS + p.batch) * p.kv_heads, rows = all < ROWS ? all : ROWS;
-  return launch_pdl(packed_combine_kernel<T, HD, ROWS>, dim3((unsigned)pairs, (unsigned)((rows + kRows - 1) / kRows)),
+  const long long all = p.q_rows * p.group, items = (all < ROWS ? all : ROWS) * (HD / 4);
+  return launch_pdl(packed_combine_kernel<T, HD, ROWS>,
+                    dim3((unsigned)(p.n_ctas - 1), (unsigned)((items + kCombineThreads * kItems - 1) / (kCombineThreads * kItems))),
                     dim3(kCombineThreads), 0, st, 1, p);
+}
+
+template <typename T, int BQ>
+cudaError_t launch_simt_hd(const PackedParams& p, int head_dim, cudaStream_t st) {
+  switch (head_dim) {
+    case 32: return launch_simt_as<T, 32, BQ>(p, st);
+    case 64: return launch_simt_as<T, 64, BQ>(p, st);
+    case 128: return launch_simt_as<T, 128, BQ>(p, st);
+    default: return launch_simt_as<T, 256, BQ>(p, st);
+  }
+}
+template <typename T, int BQ>
+cudaError_t launch_combine_hd(const PackedParams& p, int head_dim, cudaStream_t st) {
+  switch (head_dim) {
+    case 32: return launch_combine_as<T, 32, BQ>(p, st);
+    case 64: return launch_combine_as<T, 64, BQ>(p, st);
+    case 128: return launch_combine_as<T, 128, BQ>(p, st);
+    default: return launch_combine_as<T, 256, BQ>(p, st);
+  }
 }
 }  // namespace
 
-cudaError_t launch_packed_simt(const PackedParams& p, int head_dim, bool bf16, cudaStream_t st) {
-  switch (head_dim) {
-    case 32: return bf16 ? launch_simt_as<__nv_bfloat16, 32>(p, st) : launch_simt_as<float, 32>(p, st);
-    case 64: return bf16 ? launch_simt_as<__nv_bfloat16, 64>(p, st) : launch_simt_as<float, 64>(p, st);
-    case 128: return bf16 ? launch_simt_as<__nv_bfloat16, 128>(p, st) : launch_simt_as<float, 128>(p, st);
-    default: return bf16 ? launch_simt_as<__nv_bfloat16, 256>(p, st) : launch_simt_as<float, 256>(p, st);
-  }
+cudaError_t launch_packed_simt(const PackedParams& p, int head_dim, int bq, bool bf16, cudaStream_t st) {
+  if (bq == kSimtRows) return bf16 ? launch_simt_hd<__nv_bfloat16, kSimtRows>(p, head_dim, st) : launch_simt_hd<float, kSimtRows>(p, head_dim, st);
+  return bf16 ? launch_simt_hd<__nv_bfloat16, kSimtFewRows>(p, head_dim, st) : launch_simt_hd<float, kSimtFewRows>(p, head_dim, st);
 }
 
 cudaError_t launch_packed_combine(const PackedParams& p, int head_dim, int bq, bool bf16, cudaStream_t st) {
   if (bq == kTcRows)
     return head_dim == 128 ? launch_combine_as<__nv_bfloat16, 128, kTcRows>(p, st) : launch_combine_as<__nv_bfloat16, 64, kTcRows>(p, st);
-  switch (head_dim) {
-    case 32: return bf16 ? launch_combine_as<__nv_bfloat16, 32, kSimtRows>(p, st) : launch_combine_as<float, 32, kSimtRows>(p, st);
-    case 64: return bf16 ? launch_combine_as<__nv_bfloat16, 64, kSimtRows>(p, st) : launch_combine_as<float, 64, kSimtRows>(p, st);
-    case 128: return bf16 ? launch_combine_as<__nv_bfloat16, 128, kSimtRows>(p, st) : launch_combine_as<float, 128, kSimtRows>(p, st);
-    default: return bf16 ? launch_combine_as<__nv_bfloat16, 256, kSimtRows>(p, st) : launch_combine_as<float, 256, kSimtRows>(p, st);
-  }
+  if (bq == kSimtRows)
+    return bf16 ? launch_combine_hd<__nv_bfloat16, kSimtRows>(p, head_dim, st) : launch_combine_hd<float, kSimtRows>(p, head_dim, st);
+  return bf16 ? launch_combine_hd<__nv_bfloat16, kSimtFewRows>(p, head_dim, st) : launch_combine_hd<float, kSimtFewRows>(p, head_dim, st);
 }
 
 }  // namespace dare

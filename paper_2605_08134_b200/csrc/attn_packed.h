@@ -15,7 +15,8 @@
 
 namespace dare {
 
-constexpr int kUnitKeys = 128;
+// A unit is 2^kUnitShift keys, more where the line would have 2^31 of them.
+constexpr int kUnitShift = 7;
 
 struct PackedParams {
   const void* q;
@@ -33,8 +34,9 @@ struct PackedParams {
   long long q_rows, k_rows;
   int batch, n_heads, kv_heads, group, causal;
   float scale_log2;              // scale * log2(e)
+  int unit_shift;                // log2 of the keys of a unit
+  unsigned group_magic;          // ceil(2^24 / group)
   int n_ctas;                    // CTAs of the shares launch
-  int min_units;                 // a share has at least so many
   int k_head_inner, v_head_inner; // tensor maps: dimension 1 is the head (else the row)
 };
 
@@ -68,22 +70,40 @@ __device__ __forceinline__ int keys_seen(const PackedParams& p, const SeqGeom& s
 struct Place {
   SeqGeom s;
   int tiles, h, tile;            // tiles of the sequence; head and tile of the pair
-  int units;                     // of each of its pairs (shares)
-  long long first;               // unit of the launch's line where the pair begins
+  unsigned units;                // the pair's (shares)
+  unsigned first;                // unit of the launch's line where the pair begins
 };
 
-__device__ __forceinline__ long long divide(long long a, int b) {       // (64-bit divisions cost ten times as much)
-  return a <= 0x7fffffffll ? (long long)((unsigned)a / (unsigned)b) : a / b;
-}
+// Units before tile T of a head.  Without a mask every tile has ceil(n / unit).  Causal: the last row of tile t is row (t + 1) BQ - 1 of
+// the packed rows, query (that) / G, which sees n - nq more keys than its number plus one; as BQ divides unit * G = band * BQ, its
+// units are floor((t + e) / band) + 1 with e = ceil((n - nq) G / BQ) = q0 band + r0, one at least (a tile that sees no key still
+// writes its rows; the last tile may count a unit it does not have), and their sum is that of an arithmetic series in steps of
+// `band` tiles.
+struct UnitCount {
+  unsigned per_tile;             // 1 + q0; no mask: units of every tile
+  unsigned band;                 // 0: no mask
+  int r0;                        // at most band; negative where the first queries see no key
+  __device__ __forceinline__ unsigned before(int T) const {
+    unsigned units = (unsigned)T * per_tile;
+    if (band != 0 && T + r0 > 0) {                                            // + sum of floor(i / band) over i < T + r0
+      const unsigned x = (unsigned)(T + r0), q = x / band, r = x - q * band;
+      units += band * ((q * (q - 1)) >> 1) + q * r;
+    }
+    return units;
+  }
+};
 
 // The launch's line of pairs, as a warp looks places up in it.  UNITS: a pair counts as its units of keys, else as one.  Lane l holds
-// sequence l of the 32 looked at last, so that with at most 32 sequences the lengths are read once.
+// sequence l of the 32 looked at last, so that with at most 32 sequences the lengths are read once.  Everything in 32 bits (the host
+// sees to it that the line is no longer): this is on the way to a CTA's first key, and fetching the instructions of 64-bit
+// divisions through the L2 behind other CTAs' keys took some of them 4 us.
 template <int BQ, bool UNITS>
 struct Line {
   const PackedParams& p;
   SeqGeom s;
-  int tiles, units, b0;          // of this lane's sequence; first sequence of the 32
-  long long base, mine, inc;     // units before the 32; of this lane's sequence; up to and with it
+  int tiles, b0;                 // of this lane's sequence; first sequence of the 32
+  UnitCount count;
+  unsigned base, head, inc;      // units before the 32; of a head of this lane's sequence; up to and with its last head
 
   __device__ __forceinline__ explicit Line(const PackedParams& p_) : p(p_) {
     load(0);
@@ -94,13 +114,27 @@ struct Line {
     b0 = first;
     s = SeqGeom{0, 0, 0, 0};
     if (b < p.batch) s = seq_geom(p, b);
-    tiles = (int)(((long long)s.nq * p.group + BQ - 1) / BQ);
-    units = UNITS ? max(1, (s.n + kUnitKeys - 1) / kUnitKeys) : 1;
-    mine = (long long)tiles * p.kv_heads * units;
-    inc = mine;
+    tiles = (int)(((unsigned)s.nq * (unsigned)p.group + BQ - 1) / BQ);
+    head = (unsigned)tiles;
+    if (UNITS) {
+      const int shift = p.unit_shift, d = s.n - s.nq;
+      if (p.causal) {
+        count.band = (unsigned)p.group << (shift - kLogBq);
+        count.per_tile = 1u + (d > 0 ? (unsigned)d >> shift : 0u);
+        count.r0 = d > 0 ? (int)(((unsigned)(d & ((1 << shift) - 1)) * (unsigned)p.group + BQ - 1) >> kLogBq)
+                         : -(int)(((unsigned)-d * (unsigned)p.group) >> kLogBq);
+      } else {
+        const unsigned units = ((unsigned)s.n + (1u << shift) - 1) >> shift;
+        count.band = 0;
+        count.per_tile = units > 1 ? units : 1;
+        count.r0 = 0;
+      }
+      head = count.before(tiles);
+    }
+    inc = head * (unsigned)p.kv_heads;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+      const unsigned v = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += v;
     }
   }
@@ -115,61 +149,94 @@ struct Line {
     if (b0 != 0) load(0);
     base = 0;
   }
-  __device__ __forceinline__ long long total() {
+  __device__ __forceinline__ unsigned total() {
     rewind();
     while (next()) {}
     return base + __shfl_sync(0xffffffffu, inc, 31);
   }
   // Pair that holds unit u; the same for all lanes.  false: u is behind the last one.
-  __device__ __forceinline__ bool find(long long u, Place* out) {
+  __device__ __forceinline__ bool find(unsigned u, Place* out) {
     if (u < base) rewind();
     unsigned hit;
     while ((hit = __ballot_sync(0xffffffffu, u < base + inc)) == 0u)
       if (!next()) return false;
     const int src = __ffs((int)hit) - 1;
-    const long long begin = base + __shfl_sync(0xffffffffu, inc - mine, src);
-    place(src, begin, divide(u - begin, __shfl_sync(0xffffffffu, units, src)), out);
-    return true;
-  }
-  // Pair number `pair` of lane src's sequence, whose units begin at `begin`.
-  __device__ __forceinline__ void place(int src, long long begin, long long pair, Place* out) {
     out->s.q0 = __shfl_sync(0xffffffffu, s.q0, src);
     out->s.nq = __shfl_sync(0xffffffffu, s.nq, src);
     out->s.k0 = __shfl_sync(0xffffffffu, s.k0, src);
     out->s.n = __shfl_sync(0xffffffffu, s.n, src);
     out->tiles = __shfl_sync(0xffffffffu, tiles, src);
-    out->units = __shfl_sync(0xffffffffu, units, src);
-    out->h = (int)divide(pair, out->tiles);                            // head by head
-    const int t = (int)(pair - (long long)out->h * out->tiles);
-    // shares: first, last, second, last but one ... (causal tiles cost in proportion to their place: any two in a row cost
-    // the same); tiles: the longest first
-    out->tile = UNITS ? ((t & 1) ? out->tiles - 1 - (t >> 1) : (t >> 1)) : out->tiles - 1 - t;
-    out->first = begin + pair * out->units;
+    const unsigned per_head = __shfl_sync(0xffffffffu, head, src);
+    const unsigned in_seq = u - base - __shfl_sync(0xffffffffu, inc - head * (unsigned)p.kv_heads, src);
+    out->h = (int)(in_seq / per_head);                                        // head by head
+    const unsigned in_head = in_seq - (unsigned)out->h * per_head;
+    if (!UNITS) {
+      out->tile = out->tiles - 1 - (int)in_head;                              // the longest first
+      out->units = 1;
+      out->first = u;
+      return true;
+    }
+    if (out->tiles == 1) {
+      out->tile = 0;
+      out->units = per_head;
+      out->first = u - in_head;
+      return true;
+    }
+    UnitCount c;
+    c.per_tile = __shfl_sync(0xffffffffu, count.per_tile, src);
+    c.band = __shfl_sync(0xffffffffu, count.band, src);
+    c.r0 = __shfl_sync(0xffffffffu, count.r0, src);
+    // last tile with no more than in_head units before it: 32 guesses at a time
+    int lo = 0, span = out->tiles;
+    const int lane = threadIdx.x & 31;
+    while (span > 1) {
+      const int step = (span + 31) >> 5, t = lo + lane * step;
+      const unsigned ok = __ballot_sync(0xffffffffu, t < lo + span && c.before(t) <= in_head);       // (lane 0 always)
+      const int l = 31 - __clz((int)ok);
+      span = min(step, span - l * step);
+      lo += l * step;
+    }
+    out->tile = lo;
+    const unsigned mine = c.before(lo + (lane & 1));                          // (lanes 0 and 1)
+    const unsigned before = __shfl_sync(0xffffffffu, mine, 0);
+    out->units = __shfl_sync(0xffffffffu, mine, 1) - before;
+    out->first = u - (in_head - before);
+    return true;
   }
+  static constexpr int kLogBq = BQ == 8 ? 3 : (BQ == 32 ? 5 : (BQ == 128 ? 7 : 8));
+  static_assert(BQ == 1 << kLogBq, "rows of a tile");
 };
 // units of a share
-template <int BQ>
-__device__ __forceinline__ long long share_units(const PackedParams& p, long long total) {
-  const long long per = divide(total + p.n_ctas - 1, p.n_ctas);
-  return per < p.min_units ? p.min_units : per;
+__device__ __forceinline__ unsigned share_units(const PackedParams& p, unsigned total) {
+  return total <= (unsigned)p.n_ctas ? 1u : (total + (unsigned)p.n_ctas - 1) / (unsigned)p.n_ctas;
 }
-// Row of a tile -> its place in q, out and lse.
+
+// Row of a tile -> its place in q, out and lse: row = first query's rows before it + row of the tile.  Tiles begin at query
+// row0 / G; the small remainder is divided by a multiplication (x < 2^13, G < 2^11: exact).
+struct TileRows {
+  int query0, rest;              // row0 / G, row0 % G
+};
 struct RowAt {
   int query, head;               // of the sequence, of all heads
 };
-__device__ __forceinline__ RowAt row_at(const PackedParams& p, const Place& pl, int row) {
-  const int qi = row / p.group;
-  return RowAt{qi, pl.h * p.group + row - qi * p.group};
+__device__ __forceinline__ TileRows tile_rows(const PackedParams& p, int row0) {
+  const int q = (int)((unsigned)row0 / (unsigned)p.group);
+  return TileRows{q, row0 - q * p.group};
+}
+__device__ __forceinline__ RowAt row_at(const PackedParams& p, const TileRows& t, int h, int row) {
+  const unsigned x = (unsigned)(t.rest + row);
+  const int qi = (int)(((unsigned long long)x * p.group_magic) >> 24);
+  return RowAt{t.query0 + qi, h * p.group + (int)x - qi * p.group};
 }
 #endif
 
 // bf16, heads of 64 or 128, operands TMA can read (attn_packed_tc.cu); tiles: 256 rows a CTA, else shares
 cudaError_t launch_packed_tc(const PackedParams& p, int head_dim, bool tiles, cudaStream_t st);
-// any type, head width and alignment on the CUDA cores (attn_packed.cu), in shares
-cudaError_t launch_packed_simt(const PackedParams& p, int head_dim, bool bf16, cudaStream_t st);
+// any type, head width and alignment on the CUDA cores (attn_packed.cu), in shares; bq: kSimtRows or kSimtFewRows rows a tile
+cudaError_t launch_packed_simt(const PackedParams& p, int head_dim, int bq, bool bf16, cudaStream_t st);
 // merges what the shares left (attn_packed.cu); bq: rows of their tiles
 cudaError_t launch_packed_combine(const PackedParams& p, int head_dim, int bq, bool bf16, cudaStream_t st);
-constexpr int kTcRows = 128, kSimtRows = 32;
+constexpr int kTcRows = 128, kSimtRows = 32, kSimtFewRows = 8;
 constexpr int kSimtCtas = 2 * kSms;             // shares of the CUDA-core kernel: two CTAs an SM
 
 }  // namespace dare

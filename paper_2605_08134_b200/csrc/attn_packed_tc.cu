@@ -70,7 +70,7 @@ __device__ __forceinline__ void load_block(uint8_t* dst, const CUtensorMap* tm, 
 // What a CTA does with one pair, or a part of its keys.
 struct Segment {
   Place pl;
-  int row0;                      // first row of the CTA's tile in the sequence's rows
+  TileRows at;                   // where the CTA's rows begin
   int rows;                      // its rows (at most 128; tiles: 256)
   int blk0, n_blk;               // 64-key blocks [blk0, blk0 + n_blk)
   int slot;                      // < 0: the rows' keys are all here; else the slot of the partial result
@@ -79,21 +79,21 @@ struct Segment {
 // rows and last visible block of 128-row tile `st` of the segment
 __device__ __forceinline__ int stream_rows(const Segment& g, int st) { return max(0, min(BQ, g.rows - st * BQ)); }
 __device__ __forceinline__ int blocks_seen(const PackedParams& p, const Segment& g, int last_row) {
-  return (keys_seen(p, g.pl.s, (g.row0 + last_row) / p.group) + BK - 1) / BK;
+  return (keys_seen(p, g.pl.s, row_at(p, g.at, 0, last_row).query) + BK - 1) / BK;
 }
 
 // The segment of a share that begins at unit u (shares), or CTA u's pair (tiles); *end: unit behind it.  By a warp.
 template <bool TILES>
 using WorkLine = Line<TILES ? 2 * BQ : BQ, !TILES>;
 template <bool TILES>
-__device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, long long u, long long share_begin, long long share_end, Segment* g,
-                                           long long* end) {
+__device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, unsigned u, unsigned share_begin, unsigned share_end, Segment* g,
+                                           unsigned* end) {
   const PackedParams& p = line.p;
   if (!line.find(u, &g->pl)) return false;
   constexpr int ROWS = TILES ? 2 * BQ : BQ;
-  g->row0 = g->pl.tile * ROWS;
-  const long long left = (long long)g->pl.s.nq * p.group - g->row0;
-  g->rows = left < ROWS ? (int)left : ROWS;
+  const int row0 = g->pl.tile * ROWS;
+  g->at = tile_rows(p, row0);
+  g->rows = min(ROWS, g->pl.s.nq * p.group - row0);
   const int seen = blocks_seen(p, *g, g->rows - 1);
   if (TILES) {
     g->blk0 = 0;
@@ -101,11 +101,11 @@ __device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, long long u, l
     g->slot = -1;
     *end = u + 1;
   } else {
-    const long long pair_end = g->pl.first + g->pl.units;
-    *end = pair_end < share_end ? pair_end : share_end;
-    g->blk0 = (int)(u - g->pl.first) * (kUnitKeys / BK);
-    const int blk1 = min(seen, (int)(*end - g->pl.first) * (kUnitKeys / BK));
-    g->n_blk = max(0, blk1 - g->blk0);
+    const unsigned pair_end = g->pl.first + g->pl.units;
+    *end = min(pair_end, share_end);
+    const int shift = p.unit_shift - 6;                                      // (blocks of 64 keys)
+    g->blk0 = (int)((u - g->pl.first) << shift);
+    g->n_blk = max(0, min(seen, (int)((*end - g->pl.first) << shift)) - g->blk0);
     const bool whole = u == g->pl.first && *end == pair_end;
     g->slot = whole ? -1 : 2 * (int)blockIdx.x + (g->pl.first <= share_begin ? 0 : 1);
   }
@@ -158,12 +158,12 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   const uint32_t tmem_base = *tmem_slot;
 
   // this CTA's part of the launch's line of units (tiles: pair blockIdx.x)
-  long long share_begin = blockIdx.x, share_end = (long long)blockIdx.x + 1;
+  unsigned share_begin = blockIdx.x, share_end = blockIdx.x + 1;
   auto find_share = [&](WorkLine<TILES>& line) {
     if (TILES) return;
-    const long long total = line.total(), per = share_units<BQ>(p, total);
-    share_begin = (long long)blockIdx.x * per;
-    share_end = share_begin + per < total ? share_begin + per : total;
+    const unsigned total = line.total(), per = share_units(p, total);
+    share_begin = blockIdx.x * per;
+    share_end = min(share_begin + per, total);
   };
 
   const int st = warp < 4 ? (warp & 1) : ((warp - 4) >> 2);                  // stream
@@ -173,7 +173,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       WorkLine<TILES> line(p);
       find_share(line);
       Segment g;
-      long long u = share_begin, next;
+      unsigned u = share_begin, next;
       uint32_t cnt = 0;
       for (; u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next); u = next) {
         const int n = TILES ? g.n_blk : (g.n_blk - st + 1) / 2;
@@ -195,7 +195,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     // (warp 2 looks the segments up; the others get them through shared memory)
     WorkLine<TILES> line(p);
     if (warp == 2) find_share(line);
-    long long u = share_begin, next = 0;
+    unsigned u = share_begin, next = 0;
     uint32_t cnt = 0;                        // blocks of this stream so far: score buffer cnt & 1
     uint32_t kcnt = 0;                       // ring position (tiles: blocks of both streams)
     for (;;) {
@@ -224,7 +224,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR;
           qv[i] = make_uint4(0u, 0u, 0u, 0u);
           if (w < units && r < g.rows) {
-            const RowAt at = row_at(p, g.pl, g.row0 + r);
+            const RowAt at = row_at(p, g.at, g.pl.h, r);
             qv[i] = __ldcg(reinterpret_cast<const uint4*>(q + (long long)(g.pl.s.q0 + at.query) * p.q_token + at.head * p.q_head + unit * 8));
           }
         }
@@ -240,7 +240,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
 
       const int rows = TILES ? stream_rows(g, st) : g.rows;            // of this stream
-      const int tile_row = g.row0 + (TILES ? st * BQ : 0);
       // blocks of this stream; tiles: of the g.n_blk that pass through the ring
       const int n_st = TILES ? (rows > 0 ? min(g.n_blk, blocks_seen(p, g, st * BQ + rows - 1)) : 0) : (g.n_blk - st + 1) / 2;
       if (warp < 4) {
@@ -316,7 +315,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
         const float c = p.scale_log2;
         const bool warp_has_rows = quarter * 32 < rows;
-        const RowAt at = row_at(p, g.pl, tile_row + min(r, max(rows - 1, 0)));
+        const RowAt at = row_at(p, g.at, g.pl.h, (TILES ? st * BQ : 0) + min(r, max(rows - 1, 0)));
         const int seen = keys_seen(p, g.pl.s, at.query);
         float m = -INFINITY, l = 0.f;               // maximum the exponentials are taken against; sum against it
         for (int j = 0; j < n_st; ++j) {

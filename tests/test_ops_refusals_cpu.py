@@ -72,8 +72,8 @@ def test_attention(dare):
     for kw in (dict(struct_size=4), dict(dtype=9), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf)):
         assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
     for kw in (dict(batch=0), dict(batch=65537), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(head_dim=48),
-               dict(q_rows=-1), dict(q_rows=(1 << 24) + 1), dict(k_rows=-1), dict(k_rows=1 << 31), dict(k_token=-1), dict(v_head=1 << 38),
-               dict(o_head=127), dict(o_token=127), dict(q_rows=1 << 24, n_heads=512)):
+               dict(q_rows=-1), dict(q_rows=(1 << 24) + 1), dict(k_rows=-1), dict(k_rows=(1 << 30) + 1), dict(k_token=-1), dict(v_head=1 << 38),
+               dict(o_head=127), dict(o_token=127), dict(q_rows=1 << 24, n_heads=128)):
         assert call(_with(good, **kw)) == dare.ERR_SHAPE and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(qb=None), dict(kb=None), dict(out=None), dict(work=None)):
         assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
