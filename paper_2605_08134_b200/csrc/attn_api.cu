@@ -8,6 +8,10 @@ using namespace dare;
 namespace {
 
 constexpr int kMaxHeads = 1024;
+// Cost of a pair besides its keys, in units of 128 keys.  Sixteen tokens over 16k keys / a block of 160 over 2500, us: with 2 110.8 / 24.4,
+// 3 110.8 / 24.7, 5 111.4 / 25.9, 7 112.5 / 26.6; 4000 causal tokens of 4 and 1 heads: 77 with 0, 44 with 5.  CUDA cores, three causal
+// prompts / blocks of 62 over 910: 0 30.5 / 53.3, 1 32.2 / 50.0, 2 32.9 / 54.8.
+constexpr unsigned kPairCostTc = 3, kPairCostSimt = 1;
 
 bool valid_config(const dare_attention_config_t* c) {
   if (!c || c->struct_size != sizeof(dare_attention_config_t)) return false;
@@ -78,14 +82,26 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   p.n_ctas = tc ? kSms : kSimtCtas;
   p.group_magic = ((1u << 24) + p.group - 1) / p.group;
   p.unit_shift = kUnitShift;
-  while ((all / rows + c->batch) * c->n_kv_heads >= ((int64_t)1 << 31) / ((c->k_rows >> p.unit_shift) + 2)) ++p.unit_shift;
+  p.pair_cost = tc ? kPairCostTc : kPairCostSimt;
+  while ((all / rows + c->batch) * c->n_kv_heads >= ((int64_t)1 << 31) / ((c->k_rows >> p.unit_shift) + 2 + p.pair_cost)) ++p.unit_shift;
   p.part_ml = reinterpret_cast<float2*>(workspace);
   p.part_o = reinterpret_cast<float*>(p.part_ml + part_rows(tc));
 
   cudaError_t e;
   if (tc) {
-    // 256 rows a CTA where the sequences have more than one tile's rows on average and that fills the device, shares otherwise.
-    const bool tiles = all > (int64_t)kTcRows * c->batch && (all / 256) * c->n_kv_heads >= 3 * kSms / 4;
+    // 256 rows a CTA, or shares?  What each takes, in us, from k_rows / batch keys a sequence (a cache may hold fewer): a CTA of the first
+    // takes 2 us a 128 keys (1.2 with rows for one stream only), the launch 6; the shares take 1.1 us a 128 keys and tile of 128 rows
+    // (0.75 with few rows) over all SMs, five such for a tile itself, and 13 with the merge.  Tiles / shares in us, heads of 128, 32
+    // query and 8 key heads: a prompt of 300 tokens 12.4 / 18.0, 4000 148 / 167, four of up to 1500 81 / 102; 4 and 1 heads: 4000
+    // tokens 62 / 44; two blocks of 256 tokens over 8192 keys 124 / 78, four of 512 151 / 173, one token over 4000 keys 42 / 17, four
+    // over 200 8.4 / 11.  Of 64 such shapes (heads of 64 too) the rule takes the slower form, by more than 5 %, in six, by 33 % at most.
+    const float keys = (float)(c->k_rows / c->batch) / 128.f + 1.f;
+    const int64_t rows_each = all / c->batch;
+    const float ctas = (float)((all / 256 > c->batch ? all / 256 : c->batch) * c->n_kv_heads);
+    const float pairs = (float)((all / 128 > c->batch ? all / 128 : c->batch) * c->n_kv_heads);
+    const float tiles_us = (6.f + keys * (rows_each > 128 ? 2.f : 1.2f)) * fmaxf(1.f, ctas / (float)kSms);
+    const float shares_us = 13.f + pairs * (keys + 5.f) * (rows_each > 64 ? 1.1f : 0.75f) / (float)kSms;
+    const bool tiles = (rows_each > 128 && ctas >= (float)kSms) || tiles_us <= shares_us;
     e = launch_packed_tc(p, c->head_dim, tiles, st);
     if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);
   } else {

@@ -81,11 +81,11 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
     const Place pl = pl_sh;
     const int row0 = pl.tile * BQ, rows = min(BQ, pl.s.nq * p.group - row0);
     const TileRows tr = tile_rows(p, row0);
-    const unsigned pair_end = pl.first + pl.units, end = min(pair_end, share_end);
-    const bool whole = u == pl.first && end == pair_end;
-    const int slot = whole ? -1 : 2 * (int)blockIdx.x + (pl.first <= share_begin ? 0 : 1);
+    const Part part = part_of(pl, u, share_begin, share_end, (int)blockIdx.x);
+    if (part.k1 == 0) break;                     // (the share ends before the pair's keys begin)
+    const int slot = part.slot;
     const int last_seen = keys_seen(p, pl.s, row_at(p, tr, 0, rows - 1).query);
-    const int key0 = (int)((u - pl.first) << p.unit_shift), key1 = min(last_seen, (int)((end - pl.first) << p.unit_shift));
+    const int key0 = (int)(part.k0 << p.unit_shift), key1 = min(last_seen, (int)(part.k1 << p.unit_shift));
     for (int i = tid; i < BQ * (HD / 4); i += kThreads) {
       const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -234,8 +234,10 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
           *reinterpret_cast<float2*>(res + r * HD + c * 16 * VW + tx * VW + 2 * e) = acc[i][c * (VW / 2) + e];
     }
     __syncthreads();
-    for (int i = tid; i < rows * (HD / 4); i += kThreads) {
-      const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
+    // (a warp has 4 rows x 32 columns at a time: whole sectors of the slot, whose rows lie side by side, and of the output)
+    for (int i = tid; i < (rows + 3) / 4 * HD; i += kThreads) {
+      const int chunk = i >> 5, r = chunk / (HD / 32) * 4 + ((i >> 3) & 3), d = chunk % (HD / 32) * 32 + (i & 7) * 4;
+      if (r >= rows) continue;
       float top = -INFINITY;
 #pragma unroll
       for (int g = 0; g < KG; ++g) top = fmaxf(top, sm[S::KV_OFF + g * S::BUF + BQ * HD + r]);
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
         sum = fmaf(src[BQ * HD + BQ + r], w, sum);
       }
       if (slot >= 0) {
-        *reinterpret_cast<float4*>(p.part_o + ((size_t)slot * BQ + r) * HD + d) = o;
+        reinterpret_cast<float4*>(p.part_o)[((size_t)slot * (HD / 4) + d / 4) * BQ + r] = o;
         if (d == 0) p.part_ml[(size_t)slot * BQ + r] = make_float2(top, sum);
       } else {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_simt_kernel(const PackedPa
           p.lse[(long long)(pl.s.q0 + at.query) * p.n_heads + at.head] = sum == 0.f ? -INFINITY : top * 0.69314718055994531f + logf(sum);
       }
     }
-    u = end;
+    u = part.end;
     __syncthreads();
   }
 }
@@ -282,7 +284,7 @@ cudaError_t launch_simt_as(const PackedParams& p, cudaStream_t st) {
 // ------------------------------------------------------------------------------------------------ merge
 // o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c over the shares that hold keys of the row's pair, in the order of the keys (so the
 // result does not depend on which CTA was first).  blockIdx.x is a cut between two shares; the CTAs of the first cut in a pair merge it,
-// a thread kItems times four columns of a row.  CTAs of two warps: the first 148 fit beside the CTAs of the kernel before, look their
+// a warp kItems times 4 rows x 32 columns.  CTAs of two warps: the first 148 fit beside the CTAs of the kernel before, look their
 // cut up there and only wait for its end (CTAs of 256 threads that did so afterwards, each with 8 rows of a pair, were 8 us behind it).
 constexpr int kCombineThreads = 64, kItems = 2;
 template <typename T, int HD, int ROWS>
@@ -307,19 +309,21 @@ __global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(con
   const int c0 = (int)blockIdx.x, c1 = (int)((pl.first + pl.units - 1) / per);
   const int row0 = pl.tile * ROWS, rows = min(ROWS, pl.s.nq * p.group - row0);
   const TileRows tr = tile_rows(p, row0);
-  // the first share's part is the last of that CTA (unless the share begins with this pair), the others' their first
-  const int first_slot = 2 * c0 + (pl.first > c0 * per ? 1 : 0);
-  auto slot_of = [&](int c) { return c == c0 ? first_slot : 2 * c; };
-  const int item0 = (int)blockIdx.y * (kCombineThreads * kItems) + (int)threadIdx.x;
-  if (item0 >= rows * (HD / 4)) return;
-  int r[kItems], d[kItems];                      // (past the end: the last item again, not written)
+  // the first share's part is the last of that CTA, the others' their first
+  auto slot_of = [&](int c) { return c == c0 ? 2 * c + 1 : 2 * c; };
+  // a warp takes 4 rows x 32 columns at a time: whole 32-byte sectors of the slots and of the output
+  constexpr int COLS = HD / 32;
+  const int chunks = (rows + 3) / 4 * COLS, lane = (int)threadIdx.x & 31;
+  const int chunk0 = ((int)blockIdx.y * (kCombineThreads / 32) + ((int)threadIdx.x >> 5)) * kItems;
+  if (chunk0 >= chunks) return;
+  int r[kItems], d[kItems];                      // (past the end: the last row again, not written)
   float top[kItems], sum[kItems];
   float4 o[kItems];
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
-    const int item = min(item0 + i * kCombineThreads, rows * (HD / 4) - 1);
-    r[i] = item / (HD / 4);
-    d[i] = (item % (HD / 4)) * 4;
+    const int chunk = chunk0 + i;
+    r[i] = min(chunk / COLS * 4 + (lane >> 3), rows - 1);
+    d[i] = (chunk % COLS) * 32 + (lane & 7) * 4;
     top[i] = -INFINITY;
     sum[i] = 0.f;
     o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -334,14 +338,14 @@ __global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(con
     for (int i = 0; i < kItems; ++i) {
       const size_t at = (size_t)slot_of(c) * ROWS + r[i];
       const float2 ml = __ldcg(p.part_ml + at);
-      const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * HD + d[i]));
+      const float4 a = __ldcg(reinterpret_cast<const float4*>(p.part_o) + ((size_t)slot_of(c) * (HD / 4) + d[i] / 4) * ROWS + r[i]);
       const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top[i]);
       o[i].x = fmaf(a.x, w, o[i].x); o[i].y = fmaf(a.y, w, o[i].y); o[i].z = fmaf(a.z, w, o[i].z); o[i].w = fmaf(a.w, w, o[i].w);
       sum[i] = fmaf(ml.y, w, sum[i]);
     }
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
-    if (item0 + i * kCombineThreads >= rows * (HD / 4)) break;
+    if ((chunk0 + i) / COLS * 4 + (lane >> 3) >= rows) break;
     const float inv = sum[i] == 0.f ? 0.f : 1.f / sum[i];
     const RowAt at = row_at(p, tr, pl.h, r[i]);
     T* dst = reinterpret_cast<T*>(p.o) + (long long)(pl.s.q0 + at.query) * p.o_token + at.head * p.o_head + d[i];
@@ -353,9 +357,9 @@ __global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(con
 template <typename T, int HD, int ROWS>
 cudaError_t launch_combine_as(const PackedParams& p, cudaStream_t st) {
   // (no tile has more rows than there are)
-  const long long all = p.q_rows * p.group, items = (all < ROWS ? all : ROWS) * (HD / 4);
-  return launch_pdl(packed_combine_kernel<T, HD, ROWS>,
-                    dim3((unsigned)(p.n_ctas - 1), (unsigned)((items + kCombineThreads * kItems - 1) / (kCombineThreads * kItems))),
+  constexpr int per_cta = kCombineThreads / 32 * kItems;
+  const long long all = p.q_rows * p.group, chunks = ((all < ROWS ? all : ROWS) + 3) / 4 * (HD / 32);
+  return launch_pdl(packed_combine_kernel<T, HD, ROWS>, dim3((unsigned)(p.n_ctas - 1), (unsigned)((chunks + per_cta - 1) / per_cta)),
                     dim3(kCombineThreads), 0, st, 1, p);
 }
 

@@ -28,13 +28,14 @@ struct PackedParams {
   const int* k_begin;
   const int* k_len;              // or nullptr
   int* status;
-  float* part_o;                 // shares: [2 * n_ctas slots][BQ][HD]
+  float* part_o;                 // shares: [2 * n_ctas slots][HD / 4][BQ][4]: rows side by side, as the threads that write them are
   float2* part_ml;               // [slots][BQ] (maximum of the scaled scores in log2 units, sum against it)
   long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
   long long q_rows, k_rows;
   int batch, n_heads, kv_heads, group, causal;
   float scale_log2;              // scale * log2(e)
   int unit_shift;                // log2 of the keys of a unit
+  unsigned pair_cost;            // units at the head of a pair that stand for its own cost
   unsigned group_magic;          // ceil(2^24 / group)
   int n_ctas;                    // CTAs of the shares launch
   int k_head_inner, v_head_inner; // tensor maps: dimension 1 is the head (else the row)
@@ -70,8 +71,8 @@ __device__ __forceinline__ int keys_seen(const PackedParams& p, const SeqGeom& s
 struct Place {
   SeqGeom s;
   int tiles, h, tile;            // tiles of the sequence; head and tile of the pair
-  unsigned units;                // the pair's (shares)
-  unsigned first;                // unit of the launch's line where the pair begins
+  unsigned units;                // of its keys (shares)
+  unsigned first;                // unit of the launch's line where its keys begin
 };
 
 // Units before tile T of a head.  Without a mask every tile has ceil(n / unit).  Causal: the last row of tile t is row (t + 1) BQ - 1 of
@@ -80,7 +81,7 @@ struct Place {
 // writes its rows; the last tile may count a unit it does not have), and their sum is that of an arithmetic series in steps of
 // `band` tiles.
 struct UnitCount {
-  unsigned per_tile;             // 1 + q0; no mask: units of every tile
+  unsigned per_tile;             // 1 + q0, no mask: units of every tile; and the pair's own cost
   unsigned band;                 // 0: no mask
   int r0;                        // at most band; negative where the first queries see no key
   __device__ __forceinline__ unsigned before(int T) const {
@@ -120,13 +121,13 @@ struct Line {
       const int shift = p.unit_shift, d = s.n - s.nq;
       if (p.causal) {
         count.band = (unsigned)p.group << (shift - kLogBq);
-        count.per_tile = 1u + (d > 0 ? (unsigned)d >> shift : 0u);
+        count.per_tile = p.pair_cost + 1u + (d > 0 ? (unsigned)d >> shift : 0u);
         count.r0 = d > 0 ? (int)(((unsigned)(d & ((1 << shift) - 1)) * (unsigned)p.group + BQ - 1) >> kLogBq)
                          : -(int)(((unsigned)-d * (unsigned)p.group) >> kLogBq);
       } else {
         const unsigned units = ((unsigned)s.n + (1u << shift) - 1) >> shift;
         count.band = 0;
-        count.per_tile = units > 1 ? units : 1;
+        count.per_tile = p.pair_cost + (units > 1 ? units : 1);
         count.r0 = 0;
       }
       head = count.before(tiles);
@@ -178,8 +179,8 @@ struct Line {
     }
     if (out->tiles == 1) {
       out->tile = 0;
-      out->units = per_head;
-      out->first = u - in_head;
+      out->units = per_head - p.pair_cost;
+      out->first = u - in_head + p.pair_cost;
       return true;
     }
     UnitCount c;
@@ -199,13 +200,28 @@ struct Line {
     out->tile = lo;
     const unsigned mine = c.before(lo + (lane & 1));                          // (lanes 0 and 1)
     const unsigned before = __shfl_sync(0xffffffffu, mine, 0);
-    out->units = __shfl_sync(0xffffffffu, mine, 1) - before;
-    out->first = u - (in_head - before);
+    out->units = __shfl_sync(0xffffffffu, mine, 1) - before - p.pair_cost;
+    out->first = u - (in_head - before) + p.pair_cost;
     return true;
   }
   static constexpr int kLogBq = BQ == 8 ? 3 : (BQ == 32 ? 5 : (BQ == 128 ? 7 : 8));
   static_assert(BQ == 1 << kLogBq, "rows of a tile");
 };
+// What a share has of a pair, from unit u of the line on: its key units [k0, k1) (none where the share ends before them), and where
+// they go: slot < 0: they are all of the pair's, else the slot of the partial result.
+struct Part {
+  unsigned k0, k1, end;          // end: where the next pair begins, or the share ends
+  int slot;
+};
+__device__ __forceinline__ Part part_of(const Place& pl, unsigned u, unsigned share_begin, unsigned share_end, int cta) {
+  Part t;
+  const unsigned pair_end = pl.first + pl.units;
+  t.end = min(pair_end, share_end);
+  t.k0 = u > pl.first ? u - pl.first : 0u;
+  t.k1 = t.end > pl.first ? t.end - pl.first : 0u;
+  t.slot = t.k0 == 0 && t.k1 == pl.units ? -1 : 2 * cta + (pl.first < share_begin ? 0 : 1);
+  return t;
+}
 // units of a share
 __device__ __forceinline__ unsigned share_units(const PackedParams& p, unsigned total) {
   return total <= (unsigned)p.n_ctas ? 1u : (total + (unsigned)p.n_ctas - 1) / (unsigned)p.n_ctas;

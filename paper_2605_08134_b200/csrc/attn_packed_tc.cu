@@ -67,6 +67,31 @@ __device__ __forceinline__ void load_block(uint8_t* dst, const CUtensorMap* tm, 
     tma_load_3d(dst + c * (BK * 128), tm, c * 64, head_inner ? h : row, head_inner ? row : h, bar);
 }
 
+// 32 finished rows of a warp, thread <-> row, 32 columns at a time: through shared memory (16-byte units swizzled by
+// row), from where neighbouring lanes take neighbouring units: stores straight from the threads' rows touch 32 lines each, 2 us a
+// tile of 128 rows.
+template <int COLS>
+__device__ __forceinline__ int stage_at(int row, int unit) {
+  constexpr int UPR = COLS / 8;                                       // units a row
+  return row * (COLS * 2) + ((unit ^ (row & (UPR < 8 ? UPR - 1 : 7))) << 4);
+}
+template <int COLS>
+__device__ __forceinline__ void stage_row(uint8_t* stage, int lane, int col, const float (&o)[32]) {
+#pragma unroll
+  for (int q4 = 0; q4 < 4; ++q4) *reinterpret_cast<uint4*>(stage + stage_at<COLS>(lane, col / 8 + q4)) = pack8_bf16(o + 8 * q4);
+}
+template <int COLS, typename F>
+__device__ __forceinline__ void store_rows(const uint8_t* stage, int lane, int rows, F&& row_ptr) {
+  constexpr int UPR = COLS / 8, RPI = 32 / UPR;                       // rows an instruction
+  __syncwarp();
+#pragma unroll 4
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = i * RPI + lane / UPR, unit = lane % UPR;
+    if (r < rows) reinterpret_cast<uint4*>(row_ptr(r))[unit] = *reinterpret_cast<const uint4*>(stage + stage_at<COLS>(r, unit));
+  }
+  __syncwarp();
+}
+
 // What a CTA does with one pair, or a part of its keys.
 struct Segment {
   Place pl;
@@ -74,6 +99,7 @@ struct Segment {
   int rows;                      // its rows (at most 128; tiles: 256)
   int blk0, n_blk;               // 64-key blocks [blk0, blk0 + n_blk)
   int slot;                      // < 0: the rows' keys are all here; else the slot of the partial result
+  bool none;                     // the share ends before the pair's keys begin
 };
 
 // rows and last visible block of 128-row tile `st` of the segment
@@ -99,15 +125,16 @@ __device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, unsigned u, un
     g->blk0 = 0;
     g->n_blk = seen;
     g->slot = -1;
+    g->none = false;
     *end = u + 1;
   } else {
-    const unsigned pair_end = g->pl.first + g->pl.units;
-    *end = min(pair_end, share_end);
+    const Part part = part_of(g->pl, u, share_begin, share_end, (int)blockIdx.x);
     const int shift = p.unit_shift - 6;                                      // (blocks of 64 keys)
-    g->blk0 = (int)((u - g->pl.first) << shift);
-    g->n_blk = max(0, min(seen, (int)((*end - g->pl.first) << shift)) - g->blk0);
-    const bool whole = u == g->pl.first && *end == pair_end;
-    g->slot = whole ? -1 : 2 * (int)blockIdx.x + (g->pl.first <= share_begin ? 0 : 1);
+    *end = part.end;
+    g->blk0 = (int)(part.k0 << shift);
+    g->n_blk = max(0, min(seen, (int)(part.k1 << shift)) - g->blk0);
+    g->slot = part.slot;
+    g->none = part.k1 == 0;
   }
   return true;
 }
@@ -203,7 +230,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
       if (warp == 2) {
         Segment g;
-        const bool more = u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next);
+        bool more = u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next);
+        more = more && !g.none;                                      // (nothing follows then)
         u = next;
         if (lane == 0) {
           seg_more = more ? 1 : 0;
@@ -396,10 +424,15 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           mbar_wait(&o_full[2 * st + ((cnt + j) & 1)], ((cnt + j) >> 1) & 1, p.status);
         tc_fence_after();
 
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o) + (long long)(g.pl.s.q0 + at.query) * p.o_token + at.head * p.o_head;
+        auto out_row = [&](int row) {
+          const RowAt w = row_at(p, g.at, g.pl.h, row);
+          return reinterpret_cast<__nv_bfloat16*>(p.o) + (long long)(g.pl.s.q0 + w.query) * p.o_token + w.head * p.o_head;
+        };
         float* lse = p.lse ? p.lse + (long long)(g.pl.s.q0 + at.query) * p.n_heads + at.head : nullptr;
         if (TILES) {
           if (warp_has_rows) {
+            // (over this warp's rows of the stream's Q tile: its last score product is complete)
+            uint8_t* stage = smem + S::Q_OFF + st * S::Q_BYTES + quarter * (32 * HD * 2);
             const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1
             for (int ch = 0; ch < HD / 32; ++ch) {
@@ -412,26 +445,26 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
               }
 #pragma unroll
               for (int i = 0; i < 32; ++i) o[i] *= inv;
-              if (r < rows) {
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) reinterpret_cast<uint4*>(dst + ch * 32)[q4] = pack8_bf16(o + 8 * q4);
-              }
+              stage_row<HD>(stage, lane, ch * 32, o);
             }
+            const int first = st * BQ + quarter * 32;
+            store_rows<HD>(stage, lane, rows - quarter * 32, [&](int row) { return out_row(first + row); });
             if (lse && r < rows) *lse = l == 0.f ? -INFINITY : (m * c) * 0.69314718055994531f + logf(l);
           }
         } else {
-          // ---- merge the two streams: thread (stream, row) finishes its half of the row's columns.  The statistics go where the Q
-          // tile was: both streams' last products are complete behind the first barrier.
+          // ---- merge the two streams: thread (stream, row) finishes its half of the row's columns.  The statistics and the finished
+          // rows go where the Q tile was: both streams' last products are complete behind the first barrier.
           constexpr int HC = HD / 2;
-          float2* stat = reinterpret_cast<float2*>(smem + S::Q_OFF);
+          float2* stat = reinterpret_cast<float2*>(smem + S::Q_OFF + 8 * 32 * HC * 2 - 2 * BQ * sizeof(float2));
           asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
           stat[st * BQ + r] = make_float2(m, l);
           tc_fence_before();
           asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
           tc_fence_after();
+          const float2 other = stat[(st ^ 1) * BQ + r];
+          asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");          // (the staging may lie over the statistics)
           if (warp_has_rows) {
             const int n_other = g.n_blk - n_st;
-            const float2 other = stat[(st ^ 1) * BQ + r];
             const float m_all = fmaxf(m, other.x);
             const float w_mine = m == -INFINITY ? 0.f : fast_exp2((m - m_all) * c);
             const float w_other = other.x == -INFINITY ? 0.f : fast_exp2((other.x - m_all) * c);
@@ -439,7 +472,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             const float inv = g.slot >= 0 ? 1.f : (l_row == 0.f ? 0.f : 1.f / l_row);
             const uint32_t t_mine = tmem_o + lane_addr + st * HC;
             const uint32_t t_other = tmem_base + 4 * BK + (st ^ 1) * HD + lane_addr + st * HC;
-            float* part = p.part_o + ((size_t)max(g.slot, 0) * BQ + r) * HD + st * HC;
+            uint8_t* stage = smem + S::Q_OFF + (warp - 4) * (32 * HC * 2);
+            float4* part = reinterpret_cast<float4*>(p.part_o) + ((size_t)max(g.slot, 0) * (HD / 4) + st * (HC / 4)) * BQ + r;
 #pragma unroll 1
             for (int ch = 0; ch < HC / 32; ++ch) {
               float o[32], a[32];
@@ -455,19 +489,18 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = fmaf(a[i], w_other, o[i]);
               }
-              if (r < rows) {
-                if (g.slot >= 0) {
+              if (g.slot >= 0) {
+                if (r < rows) {
 #pragma unroll
-                  for (int q4 = 0; q4 < 8; ++q4)
-                    reinterpret_cast<float4*>(part + ch * 32)[q4] = make_float4(o[4 * q4], o[4 * q4 + 1], o[4 * q4 + 2], o[4 * q4 + 3]);
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 32; ++i) o[i] *= inv;
-#pragma unroll
-                  for (int q4 = 0; q4 < 4; ++q4) reinterpret_cast<uint4*>(dst + st * HC + ch * 32)[q4] = pack8_bf16(o + 8 * q4);
+                  for (int q4 = 0; q4 < 8; ++q4) part[(ch * 8 + q4) * BQ] = make_float4(o[4 * q4], o[4 * q4 + 1], o[4 * q4 + 2], o[4 * q4 + 3]);
                 }
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= inv;
+                stage_row<HC>(stage, lane, ch * 32, o);
               }
             }
+            if (g.slot < 0) store_rows<HC>(stage, lane, rows - quarter * 32, [&](int row) { return out_row(quarter * 32 + row) + st * HC; });
             if (st == 0 && r < rows) {
               if (g.slot >= 0) p.part_ml[(size_t)g.slot * BQ + r] = make_float2(m_all * c, l_row);
               else if (lse) *lse = l_row == 0.f ? -INFINITY : (m_all * c) * 0.69314718055994531f + logf(l_row);
