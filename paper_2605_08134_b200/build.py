@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdare.so")
 SOURCES = ["api.cu", "common.cu", "simt.cu", "gemm_f32.cu", "tc.cu", "gemm_tc.cu", "gemm_persist.cu", "gemm_swiglu.cu", "attn_tc.cu", "select_large.cu", "stack.cu",
-           "rope.cu", "attn_packed.cu", "attn_packed_tc.cu", "attn_api.cu", "linear.cu",
+           "rope.cu", "attn_packed.cu", "attn_packed_tc.cu", "attn_packed_tiles.cu", "attn_api.cu", "linear.cu",
            "linear_tc.cu"]
 
 

@@ -13,9 +13,8 @@
 // P is one bf16 part with heads of 128: its rounding (2^-8 of a weight at most) leaves the output 1.41 times as far from exact as
 // storing it as bf16 does; a second part would be half as much tensor work again.  With heads of 64 it is two (16 bits), as the
 // exponentials and not the products bound those.
-#include "attn_packed.h"
+#include "attn_packed_tc.cuh"
 #include "tc.h"
-#include "tc_ptx.cuh"
 
 namespace dare {
 
@@ -23,129 +22,47 @@ using namespace ptx;
 
 namespace {
 
-constexpr int BQ = kTcRows, BK = 64, kThreads = 384, kSoftmaxThreads = 256, kWorkers = 320;   // workers: all but the producers
-constexpr uint32_t kTmemCols = 512;
-constexpr float kRescaleStep = 8.f;
-template <int HD>
-constexpr bool kSplitP = HD == 64;
-constexpr int one_cta_per_sm(int bytes) { return bytes > 117 * 1024 ? bytes : 117 * 1024; }   // (it takes all tensor memory)
+using namespace packed_tc;
 
-template <int HD, bool TILES>
+constexpr int BK = 64, kWorkers = 320;                   // keys a block; workers: all threads but the producers
+
+template <int HD>
 struct Smem {
   static constexpr int Q_BYTES = BQ * HD * 2, KV_BYTES = BK * HD * 2;
-  static constexpr int RING = TILES ? 4 : 6;              // blocks of K and of V; shares: half of them a stream
+  static constexpr int RING = 6;                         // blocks of K and of V: half of them a stream
   static constexpr int Q_OFF = 0;
-  static constexpr int K_OFF = Q_OFF + (TILES ? 2 : 1) * Q_BYTES;
+  static constexpr int K_OFF = Q_OFF + Q_BYTES;
   static constexpr int V_OFF = K_OFF + RING * KV_BYTES;
   static constexpr int BAR_OFF = V_OFF + RING * KV_BYTES;
   static constexpr int TOTAL = one_cta_per_sm(BAR_OFF + 512 + 1024);
   static_assert(TOTAL <= 232448, "shared memory of one CTA");
 };
 
-__device__ __forceinline__ float fast_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-__device__ __forceinline__ void tma_load_3d(void* smem_dst, const CUtensorMap* tmap, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-// 64 rows (keys) of a head: HD / 64 chunks of 64 columns, counted on one barrier
-template <int HD>
-__device__ __forceinline__ void load_block(uint8_t* dst, const CUtensorMap* tm, bool head_inner, int h, int row, uint64_t* bar) {
-  mbar_arrive_expect_tx(bar, BK * HD * 2);
-#pragma unroll
-  for (int c = 0; c < HD / 64; ++c)
-    tma_load_3d(dst + c * (BK * 128), tm, c * 64, head_inner ? h : row, head_inner ? row : h, bar);
-}
-
-// 32 finished rows of a warp, thread <-> row, 32 columns at a time: through shared memory (16-byte units swizzled by
-// row), from where neighbouring lanes take neighbouring units: stores straight from the threads' rows touch 32 lines each, 2 us a
-// tile of 128 rows.
-template <int COLS>
-__device__ __forceinline__ int stage_at(int row, int unit) {
-  constexpr int UPR = COLS / 8;                                       // units a row
-  return row * (COLS * 2) + ((unit ^ (row & (UPR < 8 ? UPR - 1 : 7))) << 4);
-}
-template <int COLS>
-__device__ __forceinline__ void stage_row(uint8_t* stage, int lane, int col, const float (&o)[32]) {
-#pragma unroll
-  for (int q4 = 0; q4 < 4; ++q4) *reinterpret_cast<uint4*>(stage + stage_at<COLS>(lane, col / 8 + q4)) = pack8_bf16(o + 8 * q4);
-}
-template <int COLS, typename F>
-__device__ __forceinline__ void store_rows(const uint8_t* stage, int lane, int rows, F&& row_ptr) {
-  constexpr int UPR = COLS / 8, RPI = 32 / UPR;                       // rows an instruction
-  __syncwarp();
-#pragma unroll 4
-  for (int i = 0; i < 32 / RPI; ++i) {
-    const int r = i * RPI + lane / UPR, unit = lane % UPR;
-    if (r < rows) reinterpret_cast<uint4*>(row_ptr(r))[unit] = *reinterpret_cast<const uint4*>(stage + stage_at<COLS>(r, unit));
-  }
-  __syncwarp();
-}
-
-// What a CTA does with one pair, or a part of its keys.
-struct Segment {
-  Place pl;
-  TileRows at;                   // where the CTA's rows begin
-  int rows;                      // its rows (at most 128; tiles: 256)
-  int blk0, n_blk;               // 64-key blocks [blk0, blk0 + n_blk)
-  int slot;                      // < 0: the rows' keys are all here; else the slot of the partial result
-  bool none;                     // the share ends before the pair's keys begin
-};
-
-// rows and last visible block of 128-row tile `st` of the segment
-__device__ __forceinline__ int stream_rows(const Segment& g, int st) { return max(0, min(BQ, g.rows - st * BQ)); }
-__device__ __forceinline__ int blocks_seen(const PackedParams& p, const Segment& g, int last_row) {
-  return (keys_seen(p, g.pl.s, row_at(p, g.at, 0, last_row).query) + BK - 1) / BK;
-}
-
-// The segment of a share that begins at unit u (shares), or CTA u's pair (tiles); *end: unit behind it.  By a warp.
-template <bool TILES>
-using WorkLine = Line<TILES ? 2 * BQ : BQ, !TILES>;
-template <bool TILES>
-__device__ __forceinline__ bool segment_at(WorkLine<TILES>& line, unsigned u, unsigned share_begin, unsigned share_end, Segment* g,
-                                           unsigned* end) {
+// The segment of a share that begins at unit u; *end: unit behind it.  By a warp.
+typedef Line<BQ, true> WorkLine;
+__device__ __forceinline__ bool segment_at(WorkLine& line, unsigned u, unsigned share_begin, unsigned share_end, Segment* g, unsigned* end) {
   const PackedParams& p = line.p;
   if (!line.find(u, &g->pl)) return false;
-  constexpr int ROWS = TILES ? 2 * BQ : BQ;
-  const int row0 = g->pl.tile * ROWS;
+  const int row0 = g->pl.tile * BQ;
   g->at = tile_rows(p, row0);
-  g->rows = min(ROWS, g->pl.s.nq * p.group - row0);
-  const int seen = blocks_seen(p, *g, g->rows - 1);
-  if (TILES) {
-    g->blk0 = 0;
-    g->n_blk = seen;
-    g->slot = -1;
-    g->none = false;
-    *end = u + 1;
-  } else {
-    const Part part = part_of(g->pl, u, share_begin, share_end, (int)blockIdx.x);
-    const int shift = p.unit_shift - 6;                                      // (blocks of 64 keys)
-    *end = part.end;
-    g->blk0 = (int)(part.k0 << shift);
-    g->n_blk = max(0, min(seen, (int)(part.k1 << shift)) - g->blk0);
-    g->slot = part.slot;
-    g->none = part.k1 == 0;
-  }
+  g->rows = min(BQ, g->pl.s.nq * p.group - row0);
+  const Part part = part_of(g->pl, u, share_begin, share_end, (int)blockIdx.x);
+  const int shift = p.unit_shift - 6;                                        // (blocks of 64 keys)
+  *end = part.end;
+  g->blk0 = (int)(part.k0 << shift);
+  g->n_blk = max(0, min(blocks_seen<BK>(p, *g, g->rows - 1), (int)(part.k1 << shift)) - g->blk0);
+  g->slot = part.slot;
+  g->none = part.k1 == 0;
   return true;
 }
 
 }  // namespace
 
-template <int HD, bool TILES>
+template <int HD>
 __global__ void __launch_bounds__(kThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PackedParams p) {
-  using S = Smem<HD, TILES>;
-  constexpr int RING = TILES ? S::RING : S::RING / 2;         // blocks of a ring (shares: a ring a stream)
+  using S = Smem<HD>;
+  constexpr int RING = S::RING / 2;                            // blocks of a stream's ring
   constexpr int UPR = HD / 8;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -163,8 +80,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::RING; ++i) {
-      mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], TILES ? 2 : 1);
-      mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], TILES ? 2 : 1);
+      mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1);
+      mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&s_full[i], 1); mbar_init(&o_full[i], 1); mbar_init(&p_full[i], kSoftmaxThreads / 64);
@@ -184,10 +101,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  // this CTA's part of the launch's line of units (tiles: pair blockIdx.x)
-  unsigned share_begin = blockIdx.x, share_end = blockIdx.x + 1;
-  auto find_share = [&](WorkLine<TILES>& line) {
-    if (TILES) return;
+  // this CTA's part of the launch's line of units
+  unsigned share_begin = 0, share_end = 0;
+  auto find_share = [&](WorkLine& line) {
     const unsigned total = line.total(), per = share_units(p, total);
     share_begin = blockIdx.x * per;
     share_end = min(share_begin + per, total);
@@ -195,42 +111,39 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 
   const int st = warp < 4 ? (warp & 1) : ((warp - 4) >> 2);                  // stream
   if (warp < 2) {
-    // ---- producers (tiles: warp 0)
-    if (!TILES || warp == 0) {
-      WorkLine<TILES> line(p);
-      find_share(line);
-      Segment g;
-      unsigned u = share_begin, next;
-      uint32_t cnt = 0;
-      for (; u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next); u = next) {
-        const int n = TILES ? g.n_blk : (g.n_blk - st + 1) / 2;
-        for (int j = 0; j < n; ++j, ++cnt) {
-          const int slot = (TILES ? 0 : st * RING) + (int)(cnt % RING);
-          const uint32_t freed = ((cnt / RING) & 1) ^ 1;
-          const int row = g.pl.s.k0 + (g.blk0 + (TILES ? j : 2 * j + st)) * BK;
-          mbar_wait(&k_empty[slot], freed, p.status);
-          if (elect_one()) load_block<HD>(smem + S::K_OFF + slot * S::KV_BYTES, &tm_k, p.k_head_inner, g.pl.h, row, &k_full[slot]);
-          __syncwarp();
-          mbar_wait(&v_empty[slot], freed, p.status);
-          if (elect_one()) load_block<HD>(smem + S::V_OFF + slot * S::KV_BYTES, &tm_v, p.v_head_inner, g.pl.h, row, &v_full[slot]);
-          __syncwarp();
-        }
+    // ---- producers
+    WorkLine line(p);
+    find_share(line);
+    Segment g;
+    unsigned u = share_begin, next;
+    uint32_t cnt = 0;
+    for (; u < share_end && segment_at(line, u, share_begin, share_end, &g, &next); u = next) {
+      const int n = (g.n_blk - st + 1) / 2;
+      for (int j = 0; j < n; ++j, ++cnt) {
+        const int slot = st * RING + (int)(cnt % RING);
+        const uint32_t freed = ((cnt / RING) & 1) ^ 1;
+        const int row = g.pl.s.k0 + (g.blk0 + 2 * j + st) * BK;
+        mbar_wait(&k_empty[slot], freed, p.status);
+        if (elect_one()) load_block<HD, BK>(smem + S::K_OFF + slot * S::KV_BYTES, &tm_k, p.k_head_inner, g.pl.h, row, &k_full[slot]);
+        __syncwarp();
+        mbar_wait(&v_empty[slot], freed, p.status);
+        if (elect_one()) load_block<HD, BK>(smem + S::V_OFF + slot * S::KV_BYTES, &tm_v, p.v_head_inner, g.pl.h, row, &v_full[slot]);
+        __syncwarp();
       }
     }
   } else {
     const uint32_t tmem_s = tmem_base + st * 2 * BK, tmem_o = tmem_base + 4 * BK + st * HD;
     // (warp 2 looks the segments up; the others get them through shared memory)
-    WorkLine<TILES> line(p);
+    WorkLine line(p);
     if (warp == 2) find_share(line);
     unsigned u = share_begin, next = 0;
     uint32_t cnt = 0;                        // blocks of this stream so far: score buffer cnt & 1
-    uint32_t kcnt = 0;                       // ring position (tiles: blocks of both streams)
     for (;;) {
       // everybody is through with the segment before: its Q tile, its accumulators
       asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
       if (warp == 2) {
         Segment g;
-        bool more = u < share_end && segment_at<TILES>(line, u, share_begin, share_end, &g, &next);
+        bool more = u < share_end && segment_at(line, u, share_begin, share_end, &g, &next);
         more = more && !g.none;                                      // (nothing follows then)
         u = next;
         if (lane == 0) {
@@ -243,44 +156,42 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const Segment g = seg_sh;
       // ---- Q rows -> shared memory, K-major, 128-byte swizzle
       {
-        constexpr int TILE_UNITS = BQ * UPR, QU = ((TILES ? 2 : 1) * TILE_UNITS + kWorkers - 1) / kWorkers;
-        const int units = ((g.rows + BQ - 1) / BQ) * TILE_UNITS, u0 = (int)threadIdx.x - 64;
+        constexpr int UNITS = BQ * UPR, QU = (UNITS + kWorkers - 1) / kWorkers;
+        const int u0 = (int)threadIdx.x - 64;
         const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q);
         uint4 qv[QU];
 #pragma unroll
         for (int i = 0; i < QU; ++i) {
           const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR;
           qv[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (w < units && r < g.rows) {
+          if (r < g.rows) {
             const RowAt at = row_at(p, g.at, g.pl.h, r);
             qv[i] = __ldcg(reinterpret_cast<const uint4*>(q + (long long)(g.pl.s.q0 + at.query) * p.q_token + at.head * p.q_head + unit * 8));
           }
         }
 #pragma unroll
         for (int i = 0; i < QU; ++i) {
-          const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR, rt = r & (BQ - 1);
-          if (w < units)
-            *reinterpret_cast<uint4*>(smem + S::Q_OFF + (r / BQ) * S::Q_BYTES + (unit >> 3) * (BQ * 128) + rt * 128 +
-                                      (((unit & 7) ^ (rt & 7)) << 4)) = qv[i];
+          const int w = u0 + i * kWorkers, r = w / UPR, unit = w % UPR;
+          if (w < UNITS)
+            *reinterpret_cast<uint4*>(smem + S::Q_OFF + (unit >> 3) * (BQ * 128) + r * 128 + (((unit & 7) ^ (r & 7)) << 4)) = qv[i];
         }
         fence_proxy_async_smem();
       }
       asm volatile("bar.sync 2, %0;" ::"n"(kWorkers) : "memory");
 
-      const int rows = TILES ? stream_rows(g, st) : g.rows;            // of this stream
-      // blocks of this stream; tiles: of the g.n_blk that pass through the ring
-      const int n_st = TILES ? (rows > 0 ? min(g.n_blk, blocks_seen(p, g, st * BQ + rows - 1)) : 0) : (g.n_blk - st + 1) / 2;
+      const int rows = g.rows;
+      const int n_st = (g.n_blk - st + 1) / 2;          // blocks of this stream
       if (warp < 4) {
         // ---- issuer of this stream's products
         constexpr uint32_t idesc_qk = idesc_bf16(BQ, BK, false), idesc_pv = idesc_bf16(BQ, HD, true);
-        const uint64_t q_desc = smem_desc_k_sw128(smem_u32(smem + S::Q_OFF + (TILES ? st * S::Q_BYTES : 0)));
+        const uint64_t q_desc = smem_desc_k_sw128(smem_u32(smem + S::Q_OFF));
         const uint64_t k_desc0 = smem_desc_k_sw128(smem_u32(smem + S::K_OFF));
         const uint64_t v_desc0 = smem_desc_mn_sw128(smem_u32(smem + S::V_OFF), BK * 128);
-        const int ring0 = TILES ? 0 : st * RING;
+        const int ring0 = st * RING;
         auto issue_qk = [&](int j) {
-          const uint32_t kc = kcnt + j, sb = (cnt + j) & 1;
-          const int slot = ring0 + (int)(kc % RING);
-          mbar_wait(&k_full[slot], (kc / RING) & 1, p.status);
+          const uint32_t sc = cnt + j, sb = sc & 1;
+          const int slot = ring0 + (int)(sc % RING);
+          mbar_wait(&k_full[slot], (sc / RING) & 1, p.status);
           tc_fence_after();
           if (elect_one()) {
             const uint64_t k_desc = k_desc0 + (uint64_t)(slot * (S::KV_BYTES >> 4));
@@ -296,12 +207,12 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (n_st > 0) issue_qk(0);
         if (n_st > 1) issue_qk(1);
         for (int j = 0; j < n_st; ++j) {
-          const uint32_t kc = kcnt + j, sc = cnt + j, sb = sc & 1;
-          const int slot = ring0 + (int)(kc % RING);
-          mbar_wait(&p_full[2 * st + sb], (sc >> 1) & 1, p.status);          // P(j) has replaced S(j)
-          mbar_wait(&v_full[slot], (kc / RING) & 1, p.status);
+          const uint32_t sc = cnt + j, sb = sc & 1;
+          const int slot = ring0 + (int)(sc % RING);
+          mbar_poll(&p_full[2 * st + sb], (sc >> 1) & 1, p.status);          // P(j) has replaced S(j)
+          mbar_wait(&v_full[slot], (sc / RING) & 1, p.status);
           // rows behind the sequence's last key are whatever lies there, and 0 * inf would be NaN: they become zeros
-          const int keys = g.pl.s.n - (g.blk0 + (TILES ? j : 2 * j + st)) * BK;
+          const int keys = g.pl.s.n - (g.blk0 + 2 * j + st) * BK;
           if (keys < BK) {
             uint8_t* v = smem + S::V_OFF + slot * S::KV_BYTES;
             for (int i = lane; i < (BK - keys) * UPR; i += 32) {
@@ -325,30 +236,18 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           __syncwarp();
           if (j + 2 < n_st) issue_qk(j + 2);          // (in issue order behind the product that reads P(j))
         }
-        if (TILES) {
-          for (int j = n_st; j < g.n_blk; ++j) {      // blocks that only the other stream's rows see
-            const uint32_t kc = kcnt + j;
-            const int slot = (int)(kc % RING);
-            mbar_wait(&k_full[slot], (kc / RING) & 1, p.status);
-            if (elect_one()) mbar_arrive(&k_empty[slot]);
-            __syncwarp();
-            mbar_wait(&v_full[slot], (kc / RING) & 1, p.status);
-            if (elect_one()) mbar_arrive(&v_empty[slot]);
-            __syncwarp();
-          }
-        }
       } else {
         // ---- softmax of this stream's rows
         const int quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
         const float c = p.scale_log2;
         const bool warp_has_rows = quarter * 32 < rows;
-        const RowAt at = row_at(p, g.at, g.pl.h, (TILES ? st * BQ : 0) + min(r, max(rows - 1, 0)));
+        const RowAt at = row_at(p, g.at, g.pl.h, min(r, rows - 1));
         const int seen = keys_seen(p, g.pl.s, at.query);
         float m = -INFINITY, l = 0.f;               // maximum the exponentials are taken against; sum against it
         for (int j = 0; j < n_st; ++j) {
           const uint32_t sc = cnt + j, sb = sc & 1, sbuf = tmem_s + sb * BK + lane_addr;
-          mbar_wait(&s_full[2 * st + sb], (sc >> 1) & 1, p.status);
+          mbar_poll(&s_full[2 * st + sb], (sc >> 1) & 1, p.status);
           tc_fence_after();
           if (!warp_has_rows) {                     // rows of no query: only hand the block on
             tc_fence_before();
@@ -356,7 +255,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             if (lane == 0) mbar_arrive(&p_full[2 * st + sb]);
             continue;
           }
-          const int keys = seen - (g.blk0 + (TILES ? j : 2 * j + st)) * BK;     // of the block that this row sees
+          const int keys = seen - (g.blk0 + 2 * j + st) * BK;     // of the block that this row sees
           float v[BK];
           tmem_ld_32x32_nowait(sbuf, v);
           tmem_ld_32x32_nowait(sbuf + 32, v + 32);
@@ -429,29 +328,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           return reinterpret_cast<__nv_bfloat16*>(p.o) + (long long)(g.pl.s.q0 + w.query) * p.o_token + w.head * p.o_head;
         };
         float* lse = p.lse ? p.lse + (long long)(g.pl.s.q0 + at.query) * p.n_heads + at.head : nullptr;
-        if (TILES) {
-          if (warp_has_rows) {
-            // (over this warp's rows of the stream's Q tile: its last score product is complete)
-            uint8_t* stage = smem + S::Q_OFF + st * S::Q_BYTES + quarter * (32 * HD * 2);
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
-            for (int ch = 0; ch < HD / 32; ++ch) {
-              float o[32];
-              if (n_st > 0) {
-                tmem_ld_32x32(tmem_o + lane_addr + ch * 32, o);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0.f;
-              }
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= inv;
-              stage_row<HD>(stage, lane, ch * 32, o);
-            }
-            const int first = st * BQ + quarter * 32;
-            store_rows<HD>(stage, lane, rows - quarter * 32, [&](int row) { return out_row(first + row); });
-            if (lse && r < rows) *lse = l == 0.f ? -INFINITY : (m * c) * 0.69314718055994531f + logf(l);
-          }
-        } else {
+        {
           // ---- merge the two streams: thread (stream, row) finishes its half of the row's columns.  The statistics and the finished
           // rows go where the Q tile was: both streams' last products are complete behind the first barrier.
           constexpr int HC = HD / 2;
@@ -510,7 +387,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
       }
       cnt += n_st;
-      kcnt += TILES ? g.n_blk : n_st;
     }
   }
   tc_fence_before();
@@ -518,36 +394,32 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   if (warp == 2) tmem_dealloc(tmem_base, kTmemCols);
 }
 
-namespace {
-// [rows][heads][head_dim] with any strides as a tensor map of boxes 64 columns x 64 rows of one head; the dimension with the smaller
-// stride comes first.  A dimension of one entry has no stride of its own.
+// [rows][heads][head_dim] with any strides as a tensor map of boxes 64 columns x `keys` rows of one head; the dimension with the
+// smaller stride comes first.  A dimension of one entry has no stride of its own.
 bool make_head_map(CUtensorMap* m, const void* base, int head_dim, uint64_t heads, uint64_t rows, long long head_stride, long long row_stride,
-                   int* head_inner) {
+                   int keys, int* head_inner) {
   if (heads == 1) head_stride = head_dim;
   if (rows == 1) row_stride = head_stride * (long long)heads;
   *head_inner = head_stride <= row_stride ? 1 : 0;
   return make_map_3d(m, base, head_dim, *head_inner ? heads : rows, *head_inner ? rows : heads, *head_inner ? head_stride : row_stride,
-                     *head_inner ? row_stride : head_stride, *head_inner ? 1 : BK, *head_inner ? BK : 1);
+                     *head_inner ? row_stride : head_stride, *head_inner ? 1 : keys, *head_inner ? keys : 1);
 }
 
-template <int HD, bool TILES>
-cudaError_t launch_as(PackedParams p, cudaStream_t st) {
+template <int HD>
+static cudaError_t launch_shares(PackedParams p, cudaStream_t st) {
   static std::atomic<unsigned long long> attr{0};
-  auto kern = packed_tc_kernel<HD, TILES>;
-  if (cudaError_t e = ensure_dyn_smem(kern, Smem<HD, TILES>::TOTAL, attr); e != cudaSuccess) return e;
+  auto kern = packed_tc_kernel<HD>;
+  if (cudaError_t e = ensure_dyn_smem(kern, Smem<HD>::TOTAL, attr); e != cudaSuccess) return e;
   CUtensorMap mk, mv;
-  if (!make_head_map(&mk, p.k, HD, p.kv_heads, p.k_rows, p.k_head, p.k_token, &p.k_head_inner) ||
-      !make_head_map(&mv, p.v, HD, p.kv_heads, p.k_rows, p.v_head, p.v_token, &p.v_head_inner))
+  if (!make_head_map(&mk, p.k, HD, p.kv_heads, p.k_rows, p.k_head, p.k_token, BK, &p.k_head_inner) ||
+      !make_head_map(&mv, p.v, HD, p.kv_heads, p.k_rows, p.v_head, p.v_token, BK, &p.v_head_inner))
     return cudaErrorInvalidValue;
-  // tiles: as many CTAs as there can be pairs (a sequence's last tile may be partly filled); those behind the last one leave
-  const long long grid = TILES ? ((p.q_rows * p.group) / (2 * BQ) + p.batch) * p.kv_heads : p.n_ctas;
-  return launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), Smem<HD, TILES>::TOTAL, st, 1, mk, mv, p);
+  return launch_pdl(kern, dim3((unsigned)p.n_ctas), dim3(kThreads), Smem<HD>::TOTAL, st, 1, mk, mv, p);
 }
-}  // namespace
 
 cudaError_t launch_packed_tc(const PackedParams& p, int head_dim, bool tiles, cudaStream_t st) {
-  if (head_dim == 128) return tiles ? launch_as<128, true>(p, st) : launch_as<128, false>(p, st);
-  return tiles ? launch_as<64, true>(p, st) : launch_as<64, false>(p, st);
+  if (tiles) return launch_packed_tiles(p, head_dim, st);
+  return head_dim == 128 ? launch_shares<128>(p, st) : launch_shares<64>(p, st);
 }
 
 }  // namespace dare

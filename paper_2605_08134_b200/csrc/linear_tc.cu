@@ -127,7 +127,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         tc_fence_after();
         for (int kb = 0; kb < KB; ++kb, ++it) {
           const int s = it % stages;
-          mbar_wait(&full_bar[s], (it / stages) & 1, p.status);
+          mbar_poll(&full_bar[s], (it / stages) & 1, p.status);
           tc_fence_after();
           if (elect_one()) {
             const uint32_t at = smem_u32(smem + s * stage_bytes);
