@@ -1,18 +1,20 @@
-// Attention over packed sequences on tcgen05 tensor cores: bf16, head_dim 128 or 64, fp32 softmax (attn_packed.h: rows, pairs,
-// tiles and shares).
-//   warps 0, 1   TMA: K and V blocks of 64 keys (64-column boxes, 128-byte swizzle) into rings
-//   warps 2, 3   one lane each issues the products of one stream: S = Q K^T (M 128, N 64) into one of two score buffers, O += P V with
-//                P read from tensor memory
-//   warps 4-11   softmax, four warps a stream, thread <-> row: scores from tensor memory, maximum, 2^x, P as bf16 back over the
-//                scores' columns; O is rescaled in place only when a row's maximum grew by more than 2^8
-// tiles:  a CTA has 256 rows, stream s rows 128 s ..; the streams walk the same blocks and share them: half of what a CTA pulls
-//         from the L2 a flop.  Causal rows see different numbers of blocks; a stream that is through only hands the ring on.
-// shares: a CTA has 128 rows and the streams take its blocks in turn, so that few rows (a decoding step has n_heads / n_kv_heads of
-//         them) still keep 192 KB of keys and values on their way; the streams' results are merged as two parts of a key split.
-//         The producers know a share's segments themselves and run ahead into the next one while the rest of the CTA finishes.
-// P is one bf16 part with heads of 128: its rounding (2^-8 of a weight at most) leaves the output 1.41 times as far from exact as
-// storing it as bf16 does; a second part would be half as much tensor work again.  With heads of 64 it is two (16 bits), as the
-// exponentials and not the products bound those.
+// Attention over packed sequences on tcgen05 tensor cores: bf16, head_dim 128 or 64, fp32 softmax (attn_packed.h: rows, pairs, tiles and
+// shares).  Both forms have the same parts; this file has the one for few rows (shares), attn_packed_tiles.cu the one for many.
+//   TMA       K and V blocks (64-column boxes, 128-byte swizzle) into rings
+//   issuers   one lane of a warp for each of two streams: S = Q K^T into a score buffer of tensor memory, O += P V with P read from
+//             tensor memory
+//   softmax   four warps a stream, thread <-> row: scores from tensor memory, maximum, 2^x, P as bf16 back over the scores; O is rescaled
+//             in place only when a row's maximum grew by more than 2^8
+// P is one bf16 part: its rounding (2^-8 of a weight at most) leaves the output 1.3 to 1.4 times as far from exact as storing it as
+// bf16 does.  A second part for what the rounding left would bring that to 1.0, and took 10 % (a block of 160 over 2500 keys) to 30 %
+// (prompts) more time with heads of 64, half as much tensor work again with heads of 128.
+// Shares: a CTA has 128 rows and its streams take its blocks of 64 keys in turn, so that few rows (a decoding step has n_heads /
+// n_kv_heads of them) still keep 192 KB of keys and values on their way; the streams' results are merged as two parts of a key
+// split.  Two score buffers a stream: the next block's scores are there when the softmax is through with one.  The producers know a
+// share's segments themselves and run ahead into the next one while the rest of the CTA finishes.
+//   warps 0, 1 TMA; 2, 3 issuers; 4-11 softmax
+// Bound by the HBM with many keys (16 tokens over up to 16k keys each: 650 MB in 111 us, 0.89 of the copy peak); with few by the way of a
+// segment: look-up 1.7 us, rows 0.8, first scores 0.6, a unit of 128 keys 0.7, rows out 0.8 to 1.5, merge 2.5.
 #include "attn_packed_tc.cuh"
 #include "tc.h"
 
@@ -228,7 +230,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
             for (int ks = 0; ks < BK / 16; ++ks) {
               umma_ts(tmem_o, tmem_s + sb * BK + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, (j | ks) != 0 ? 1u : 0u);
-              if (kSplitP<HD>) umma_ts(tmem_o, tmem_s + sb * BK + 32 + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, 1u);
             }
             umma_commit(&o_full[2 * st + sb]);
             umma_commit(&v_empty[slot]);
@@ -296,7 +297,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const float mc = m == -INFINITY ? 0.f : m * c;             // (nothing seen yet: 2^-inf = 0, not 2^NaN)
           const float2 c2 = make_float2(c, c), nmc2 = make_float2(-mc, -mc);
           float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          float pk[BK / 2], pl[kSplitP<HD> ? BK / 2 : 1];
+          float pk[BK / 2];
 #pragma unroll
           for (int i = 0; i < BK; i += 2) {
             float2 e = __ffma2_rn(make_float2(v[i], v[i + 1]), c2, nmc2);
@@ -305,14 +306,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             sum2[(i >> 1) & 1] = __fadd2_rn(sum2[(i >> 1) & 1], e);
             __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
             pk[i >> 1] = __uint_as_float(*reinterpret_cast<uint32_t*>(&h2));
-            if (kSplitP<HD>) {
-              const float2 rest = __fadd2_rn(e, make_float2(-__low2float(h2), -__high2float(h2)));
-              __nv_bfloat162 l2 = __floats2bfloat162_rn(rest.x, rest.y);
-              pl[kSplitP<HD> ? i >> 1 : 0] = __uint_as_float(*reinterpret_cast<uint32_t*>(&l2));
-            }
           }
           tmem_st_32x32_nowait(sbuf, pk);
-          if (kSplitP<HD>) tmem_st_32x32_nowait(sbuf + 32, pl);
           tmem_st_wait();
           l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           tc_fence_before();

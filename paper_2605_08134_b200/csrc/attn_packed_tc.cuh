@@ -12,9 +12,6 @@ using namespace ptx;
 constexpr int BQ = kTcRows, kThreads = 384, kSoftmaxThreads = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kRescaleStep = 8.f;        // log2 of the growth of a row's maximum that has O rescaled
-// Two bf16 parts of P with heads of 64: see attn_packed_tc.cu
-template <int HD>
-constexpr bool kSplitP = HD == 64;
 constexpr int one_cta_per_sm(int bytes) { return bytes > 117 * 1024 ? bytes : 117 * 1024; }   // (a CTA takes all tensor memory)
 
 __device__ __forceinline__ float fast_exp2(float x) {

@@ -184,7 +184,6 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               for (int ks = 0; ks < 4; ++ks) {
                 const uint64_t v16 = v_desc + (((h * 4 + ks) * (16 * 128)) >> 4);
                 umma_ts(tmem_o, tmem_s + h * 32 + ks * 8, v16, idesc_pv, (j | h | ks) != 0 ? 1u : 0u);
-                if (kSplitP<HD>) umma_ts(tmem_o, tmem_s + 64 + h * 32 + ks * 8, v16, idesc_pv, 1u);
               }
               if (h == 1) {
                 umma_commit(&v_empty[slot]);
@@ -260,7 +259,7 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         // The exponentials are taken against the maximum of the blocks before, so that they need not wait for this one's; only if it
         // has grown by more than 2^8 (any smaller growth changes nothing in exact arithmetic) are the first half's taken again.
         float2 sum2[2];
-        float pk[16], pl[kSplitP<HD> ? 16 : 1];
+        float pk[16];
         auto exponentials = [&](auto part) {                               // of 32 keys
           constexpr int k0 = decltype(part)::value * 32;
           const float mc = m == -INFINITY ? 0.f : m * c;                   // (nothing seen yet: 2^-inf = 0, not 2^NaN)
@@ -273,17 +272,9 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             sum2[(i >> 1) & 1] = __fadd2_rn(sum2[(i >> 1) & 1], e);
             __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
             pk[i >> 1] = __uint_as_float(*reinterpret_cast<uint32_t*>(&h2));
-            if (kSplitP<HD>) {
-              const float2 rest = __fadd2_rn(e, make_float2(-__low2float(h2), -__high2float(h2)));
-              __nv_bfloat162 l2 = __floats2bfloat162_rn(rest.x, rest.y);
-              pl[kSplitP<HD> ? i >> 1 : 0] = __uint_as_float(*reinterpret_cast<uint32_t*>(&l2));
-            }
           }
         };
-        auto store_p = [&](int part) {
-          tmem_st_32x16_nowait(sbuf + part * 16, pk);
-          if (kSplitP<HD>) tmem_st_32x16_nowait(sbuf + 64 + part * 16, pl);
-        };
+        auto store_p = [&](int part) { tmem_st_32x16_nowait(sbuf + part * 16, pk); };
         auto hand_over = [&](int h) {
           tmem_st_wait();
           tc_fence_before();

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
       }
       v[0] += bv[0];
       v[1] += bv[1];
-      activate(v, p.act);
+      activate<false>(v, p.act);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         if (c[i] < p.n) {

@@ -10,11 +10,26 @@ using namespace ptx;
 namespace {
 
 // ------------------------------------------------------------------------------------------------ few rows
-// At most four rows: a stream of W.  A warp takes kOut outputs; its lanes share the k-elements, VE (16 bytes of a row that allows it)
-// a lane and step, and add their sums up at the end, halving the set of sums a lane holds at each step of the exchange.  Sums of
-// even and odd k-elements run side by side in packed multiply-adds.
+// At most four rows: a stream of W.  k_warps warps of a CTA take kOut outputs together; their lanes share the k-elements, VE (16 bytes of
+// a row that allows it) a lane and step, and add their sums up at the end, halving the set of sums a lane holds at each step of the
+// exchange.  Sums of even and odd k-elements run side by side in packed multiply-adds.  k_warps is as large as fits two
+// CTAs an SM; float32 takes four at least, where that leaves each its own batch of loads.  bf16, one row, us with 1 / 2 / 4 / 8 (the pick
+// in brackets): 4096 x 6144 [11.9] / 13.2 / 12.6 / 13.9, 4096 x 4096 10.2 / [8.0] / 9.1 / 10.4, 1024 x 1000 2.8 / 2.3 / 2.1 / [2.1], three
+// rows of 8192 x 1024 28.4 / 15.7 / 9.2 / [6.5]; float32 4096 x 6144 19.9 / 19.4 / [18.2] / 17.6, 4096 x 12288 39.4 / 32.4 / [32.2] / 30.8.
 constexpr int kOut = 4, kWarps = 8, kThreads = kWarps * 32;
 
+// 16 bytes as pairs
+template <typename T, int VE>
+__device__ __forceinline__ void widen(const uint4& raw, float2 (&v)[VE / 2]) {
+  if constexpr (sizeof(T) == 4) {
+    v[0] = make_float2(__uint_as_float(raw.x), __uint_as_float(raw.y));
+    v[1] = make_float2(__uint_as_float(raw.z), __uint_as_float(raw.w));
+  } else {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+    for (int i = 0; i < VE / 2; ++i) v[i] = __bfloat1622float2(h[i]);
+  }
+}
 // VE elements of a row from k on as pairs; past K: zeros
 template <typename T, int VE, bool WIDE>
 __device__ __forceinline__ void load_pairs(const T* row, int k, int K, float2 (&v)[VE / 2]) {
@@ -64,12 +79,13 @@ __device__ __forceinline__ void reduce_lanes(float* v, int* first) {
 }
 
 template <typename T, int MT, int VE, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearParams p) {
+__global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearParams p, const int k_warps) {
+  __shared__ float parts[kWarps][kOut * MT];
   pdl_wait();
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long n0 = (long long)blockIdx.x * (kWarps * kOut) + warp * kOut;
-  if (n0 >= p.n) return;
+  const int part = warp & (k_warps - 1), group = warp / k_warps;
+  const long long n0 = ((long long)blockIdx.x * (kWarps / k_warps) + group) * kOut;       // (past the end: the last output, not written)
   const T* x[MT];
   const T* w[kOut];
 #pragma unroll
@@ -79,20 +95,59 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
   float2 sums[kOut * MT];
 #pragma unroll
   for (int i = 0; i < kOut * MT; ++i) sums[i] = make_float2(0.f, 0.f);
-  constexpr int kUnroll = MT <= 2 ? 4 : 2;
-#pragma unroll kUnroll
-  for (int k = lane * VE; k < p.k; k += 32 * VE) {
-    float2 a[kOut][VE / 2];
+  auto multiply = [&](const float2 (&a)[VE / 2], const float2 (&b)[VE / 2], int at) {
 #pragma unroll
-    for (int j = 0; j < kOut; ++j) load_pairs<T, VE, WIDE>(w[j], k, p.k, a[j]);
+    for (int e = 0; e < VE / 2; ++e) sums[at] = __ffma2_rn(a[e], b[e], sums[at]);
+  };
+  if constexpr (WIDE) {
+    // U steps' rows of W are asked for before the first is used, and stay as they came until then
+    constexpr int U = MT <= 2 ? 4 : 2;
+    const int whole = p.k / VE, stride = k_warps * 32;
+    for (int c = part * 32 + lane; c < whole; c += U * stride) {
+      uint4 raw[U][kOut];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      float2 b[VE / 2];
-      load_pairs<T, VE, WIDE>(x[i], k, p.k, b);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < kOut; ++j)
+        for (int j = 0; j < kOut; ++j) {
+          raw[u][j] = make_uint4(0u, 0u, 0u, 0u);
+          if (c + u * stride < whole) raw[u][j] = __ldg(reinterpret_cast<const uint4*>(w[j]) + c + u * stride);
+        }
 #pragma unroll
-        for (int e = 0; e < VE / 2; ++e) sums[i * kOut + j] = __ffma2_rn(a[j][e], b[e], sums[i * kOut + j]);
+      for (int u = 0; u < U; ++u) {
+        const int at = c + u * stride;
+        if (at >= whole) break;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          float2 b[VE / 2];
+          widen<T, VE>(__ldg(reinterpret_cast<const uint4*>(x[i]) + at), b);
+#pragma unroll
+          for (int j = 0; j < kOut; ++j) {
+            float2 a[VE / 2];
+            widen<T, VE>(raw[u][j], a);
+            multiply(a, b, i * kOut + j);
+          }
+        }
+      }
+    }
+    const int k = whole * VE + lane;                               // the last few elements
+    if (part == 0 && k < p.k) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < kOut; ++j) sums[i * kOut + j].x = fmaf((float)w[j][k], (float)x[i][k], sums[i * kOut + j].x);
+    }
+  } else {
+    for (int k = (part * 32 + lane) * VE; k < p.k; k += k_warps * 32 * VE) {
+      float2 a[kOut][VE / 2];
+#pragma unroll
+      for (int j = 0; j < kOut; ++j) load_pairs<T, VE, false>(w[j], k, p.k, a[j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        float2 b[VE / 2];
+        load_pairs<T, VE, false>(x[i], k, p.k, b);
+#pragma unroll
+        for (int j = 0; j < kOut; ++j) multiply(a[j], b, i * kOut + j);
+      }
     }
   }
   float acc[kOut * MT];
@@ -102,28 +157,31 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
   int first = 0;
   reduce_lanes<N, 16>(acc, &first);
   // (fewer values than lanes: the lanes with the same ones differ in the low bits, the first of them writes)
-  if (N < 32 && (lane & (32 / (N < 32 ? N : 32) - 1)) != 0) return;
-  float v[LEFT];
+  if (N >= 32 || (lane & (32 / (N < 32 ? N : 32) - 1)) == 0) {
 #pragma unroll
-  for (int i = 0; i < LEFT; ++i) {
-    const int n = (int)n0 + (first + i) % kOut;
-    v[i] = acc[i] + (p.bias && n < p.n ? p.bias[n] : 0.f);
+    for (int i = 0; i < LEFT; ++i) parts[warp][first + i] = acc[i];
   }
-  activate(v, p.act);
-#pragma unroll
-  for (int i = 0; i < LEFT; ++i) {
-    const int m = (first + i) / kOut, n = (int)n0 + (first + i) % kOut;
-    if (m < p.rows && n < p.n) {
-      if (p.resid) v[i] += (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n];
-      reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)v[i];
-    }
-  }
+  __syncthreads();
+  const int out = (int)threadIdx.x / N, i = (int)threadIdx.x % N;              // group of outputs, value of it
+  if (out >= kWarps / k_warps) return;
+  float v[1] = {0.f};
+  for (int s = 0; s < k_warps; ++s) v[0] += parts[out * k_warps + s][i];
+  const int m = i / kOut;
+  const long long n = ((long long)blockIdx.x * (kWarps / k_warps) + out) * kOut + i % kOut;
+  if (m >= p.rows || n >= p.n) return;
+  if (p.bias) v[0] += p.bias[n];
+  activate<sizeof(T) == 2>(v, p.act);
+  if (p.resid) v[0] += (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n];
+  reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)v[0];
 }
 
 template <typename T, int MT, int VE, bool WIDE>
 cudaError_t launch_rows_as(const LinearParams& p, cudaStream_t st) {
-  return launch_pdl(linear_rows_kernel<T, MT, VE, WIDE>, dim3((unsigned)((p.n + kWarps * kOut - 1) / (kWarps * kOut))), dim3(kThreads), 0,
-                    st, 1, p);
+  int k_warps = 1;
+  while (k_warps < kWarps && (long long)p.n * k_warps * 2 <= (long long)2 * kSms * kWarps * kOut && p.k >= 2 * k_warps * 32 * VE) k_warps *= 2;
+  if (sizeof(T) == 4 && WIDE && k_warps < 4 && p.k >= 16 * 32 * VE) k_warps = 4;
+  const int outputs = kWarps / k_warps * kOut;
+  return launch_pdl(linear_rows_kernel<T, MT, VE, WIDE>, dim3((unsigned)((p.n + outputs - 1) / outputs)), dim3(kThreads), 0, st, 1, p, k_warps);
 }
 template <typename T, int VE, bool WIDE>
 cudaError_t launch_rows_by(const LinearParams& p, cudaStream_t st) {
@@ -256,7 +314,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const Line
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (p.bias && n0 + c + i < p.n) v[i] += p.bias[n0 + c + i];
-      activate(v, p.act);
+      activate<sizeof(T) == 2>(v, p.act);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int n = n0 + c + i;
@@ -270,10 +328,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const Line
   if (splits > 1) cluster_sync_all();            // nobody leaves while its sums are read
 }
 
-// Splits of the k-elements: enough CTAs for two an SM, each with at least 128 of them.
+// Splits of the k-elements: CTAs for two an SM, each with at least 128 of them.
 int pick_splits(long long tiles, int k) {
   int s = 1;
-  while (s < 8 && tiles * s * 2 <= 2 * kSms && k >= s * 2 * 128) s *= 2;
+  while (s < 8 && tiles * s * 2 <= 3 * kSms && k >= s * 2 * 128) s *= 2;
   return s;
 }
 template <typename T, int RM, bool WIDE>
@@ -329,8 +387,10 @@ cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, cudaStream_t st
 using namespace dare;
 
 namespace {
-constexpr int kRowsOnCudaCores = 4;        // bf16
-}
+// bf16: up to two rows, and up to four of a small W, go to the CUDA cores: four rows of 4096 x 6144 take 18.8 us there and 16 on the
+// tensor cores, of 4096 x 4096 12 and 14, one row of 1024 x 1000 2.0 and 5.
+bool rows_on_cuda_cores(const LinearParams& p) { return p.rows <= 2 || (p.rows <= 4 && (long long)p.n * p.k <= 20 << 20); }
+}  // namespace
 
 extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* x, const void* w, const float* bias, const void* resid,
                                      void* y, int32_t* status, void* cuda_stream) {
@@ -360,15 +420,15 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   cudaError_t e;
   if (c->dtype == DARE_BF16) {
     const bool tc = !low(x, 15u) && !low(w, 15u) && strides(c->rows, c->x_row, 8) && strides(c->out_features, c->w_row, 8);
-    e = tc && p.rows > kRowsOnCudaCores ? launch_linear_tc(p, st) : launch_linear_simt(p, true, st);
+    e = tc && !rows_on_cuda_cores(p) ? launch_linear_tc(p, st) : launch_linear_simt(p, true, st);
   } else {
     const bool aligned = !low(x, 15u) && !low(w, 15u) && c->in_features % 4 == 0 && strides(c->rows, c->x_row, 4) &&
                          strides(c->out_features, c->w_row, 4);
     // On the tensor cores a tile of 128 rows x 64 outputs takes 4.5 us and 1.1 us a block of 64 k-elements; on the CUDA cores an SM
-    // does about 70 multiply-adds a cycle and a launch takes 6 us at least.
+    // does about 50 multiply-adds a cycle and a launch takes 6 us at least.
     const int64_t tiles = (c->rows + 127) / 128 * ((c->out_features + 63) / 64);
     const float there = (float)((tiles + kSms - 1) / kSms) * (4.5f + 1.1f * (float)((c->in_features + 63) / 64)) + 2.f;
-    const float here = 6.f + (float)((c->rows + 31) / 32 * 32) * (float)c->out_features * (float)c->in_features / (70.f * 1900.f * (float)kSms);
+    const float here = 6.f + (float)((c->rows + 31) / 32 * 32) * (float)c->out_features * (float)c->in_features / (50.f * 1900.f * (float)kSms);
     e = aligned && p.rows > 4 && there < here ? launch_linear_f32(p, st) : launch_linear_simt(p, false, st);
   }
   if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }

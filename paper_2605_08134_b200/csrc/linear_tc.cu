@@ -196,7 +196,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                 if (c + i < cols) v[i] += __ldg(b + i);
             }
           }
-          activate(v, p.act);
+          activate<true>(v, p.act);
           if (row < p.rows) {
             if (full) {
               if (resid) {
@@ -228,7 +228,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
       } else if (warp_has_rows) {
         // Rows of y or resid that are not on the 16-byte grid: 16 columns at a time through 2 KB of shared memory (the rows that the
         // last stage's MMA reads past its own; units of 16 bytes swizzled by row), from where half a warp takes a row: 2-byte
-        // stores of 32 rows at a time took as long as the main loop (3080 x 6400 x 1899: 111 us).
+        // stores of 32 rows at a time took as long as the main loop (3080 x 6400 x 1899: 111 us, 64 so).
         float* stg = reinterpret_cast<float*>(smem + kRing) + (warp - 2) * (32 * 16);
         const int lr = lane >> 4, lc = lane & 15;
 #pragma unroll 1
@@ -249,7 +249,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             const int r = 2 * i + lr;
             o[i] = stg[r * 16 + ((((lc >> 2) ^ ((r >> 1) & 3)) << 2) | (lc & 3))] + bias;
           }
-          activate(o, p.act);
+          activate<true>(o, p.act);
           const long long row0 = m0 + q * 32 + lr;
           const __nv_bfloat16* rp = reinterpret_cast<const __nv_bfloat16*>(p.resid) + (p.resid ? row0 * p.resid_row + n0 + c + lc : 0);
           __nv_bfloat16* yp = reinterpret_cast<__nv_bfloat16*>(p.y) + row0 * p.y_row + n0 + c + lc;
@@ -279,7 +279,13 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
 }
 
 // Tile width and form: waves of tiles times what a k-block takes an SM (the tensor pipe's cycles, or the operand bytes
-// at 64 a cycle), plus the finishing pass of the last tile.
+// at 64 a cycle), plus the finishing pass of the last tile.  us by width, p: pairs, the pick in brackets:
+//   37 rows of 4096 x 12288   48 27.7, 64 28.5, [96 21.3], 128 21.9, 160 23.6, 192 24.2, 256 32.5
+//   256 of 4096 x 4096        64 15.8, 96 18.3, 128 19.1, [p64 15.0], p96 16.0, p128 16.3, p256 24.7
+//   256 of 4096 x 12288       96 35.9, 192 33.8, p96 30.9, p160 41.0, [p192 28.1], p224 29.5, p256 30.9
+//   512 of 4096 x 4096        96 30.7, 128 19.2, p96 25.3, [p128 16.9], p160 21.2, p256 25.0
+//   2048 of 4096 x 4096       128 64.5, 256 59.6, p128 53.6, p160 52.1, p224 59.0, [p256 49.2]
+// At the ten sizes timed (8 to 2048 rows) the pick was the fastest or within 0.4 us of it.
 struct Form { int pair, width; };
 Form pick_form(int rows, int n, int k) {
   const int m_tiles = (rows + BM - 1) / BM, KB = (k + BK - 1) / BK, x_rows = rows < BM ? (rows + 7) / 8 * 8 : BM;

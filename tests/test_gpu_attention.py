@@ -40,7 +40,7 @@ def make(lens, heads, kv_heads, hd, dtype, seed, gap=0, std=1.0, tail=3):
 def check(lens, q, k, v, q_begin, k_begin, out, lse, causal, scale, untouched):
     """Every row of every sequence, and that the rows of nobody are as they were."""
     hd, group = q.shape[2], q.shape[1] // k.shape[1]
-    bf16, two_parts = q.dtype == BF16, hd == 64
+    bf16 = q.dtype == BF16
     qb, kb = q_begin.tolist(), k_begin.tolist()
     worst = 0.0
     for b, (nq, nk) in enumerate(lens):
@@ -62,8 +62,8 @@ def check(lens, q, k, v, q_begin, k_begin, out, lse, causal, scale, untouched):
         # magnitudes; 2^x to 2^-21 and its argument's rounding, 2^-23 of up to 3 mag; the sums over the keys, 2^-23 a key or
         # block of keys, at most (nk + 16) 2^-23
         eps = (2 * hd + 16) * 2.0 ** -24 * mag + 2.0 ** -20 + (nk + 16) * 2.0 ** -23
-        # weights rounded to bf16 for the product: 2^-8 of each, or the two parts' 2^-16
-        weights = (2.0 ** -16 if two_parts else 2.0 ** -8) if bf16 else 0.0
+        # weights rounded to bf16 for the product: 2^-8 of each
+        weights = 2.0 ** -8 if bf16 else 0.0
         bound = torch.finfo(q.dtype).eps / 2 * want.abs() * (1 + eps) + (weights + eps) * size
         assert bool(((got - want).abs() <= bound).all()), (b, ((got - want).abs() / bound.clamp(min=1e-30)).max().item())
         none = want_lse == -math.inf
