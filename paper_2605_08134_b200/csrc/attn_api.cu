@@ -8,6 +8,7 @@ using namespace dare;
 namespace {
 
 constexpr int kMaxHeads = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
 // Cost of a pair besides its keys, in units of 128 keys.  Sixteen tokens over 16k keys / a block of 160 over 2500, us: with 2 110.8 / 24.4,
 // 3 110.8 / 24.7, 5 111.4 / 25.9, 7 112.5 / 26.6; 4000 causal tokens of 4 and 1 heads: 77 with 0, 44 with 5.  CUDA cores, three causal
 // prompts / blocks of 62 over 910: 0 30.5 / 53.3, 1 32.2 / 50.0, 2 32.9 / 54.8.
@@ -17,7 +18,7 @@ bool valid_config(const dare_attention_config_t* c) {
   if (!c || c->struct_size != sizeof(dare_attention_config_t)) return false;
   if (c->dtype != DARE_F32 && c->dtype != DARE_BF16) return false;
   if (c->causal != 0 && c->causal != 1) return false;
-  if (!(c->scale > 0.f) || !isfinite(c->scale)) return false;
+  if (!(c->scale > 0.f) || !isfinite(c->scale * kLog2e)) return false;
   return true;
 }
 bool shape_ok(const dare_attention_config_t* c) {
@@ -30,9 +31,7 @@ bool shape_ok(const dare_attention_config_t* c) {
   const int64_t s[8] = {c->q_token, c->q_head, c->k_token, c->k_head, c->v_token, c->v_head, c->o_token, c->o_head};
   for (int64_t v : s)
     if (v < 0 || v >= (int64_t)1 << 38) return false;
-  // (two heads or rows of the output in one place would be written twice)
-  if ((c->n_heads > 1 && c->o_head < c->head_dim) || (c->q_rows > 1 && c->o_token < c->head_dim)) return false;
-  return true;
+  return places_apart(c->q_rows, c->o_token, c->n_heads, c->o_head, c->head_dim);
 }
 bool tc_types(const dare_attention_config_t* c) { return c->dtype == DARE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }
 size_t part_rows(bool tc) { return (size_t)2 * (tc ? kSms * kTcRows : kSimtCtas * kSimtRows); }      // two slots a CTA
@@ -67,13 +66,13 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   p.v_token = c->v_token; p.v_head = c->v_head; p.o_token = c->o_token; p.o_head = c->o_head;
   p.q_rows = c->q_rows; p.k_rows = c->k_rows;
   p.batch = c->batch; p.n_heads = c->n_heads; p.kv_heads = c->n_kv_heads; p.group = c->n_heads / c->n_kv_heads; p.causal = c->causal;
-  p.scale_log2 = c->scale * 1.4426950408889634f;
+  p.scale_log2 = c->scale * kLog2e;
 
-  // The tensor-core kernel reads k and v through TMA (16-byte aligned rows and heads with strides of their own), q and out by 16
+  // The tensor-core kernel reads k and v through TMA (16-byte aligned rows and heads that do not overlap), q and out by 16
   // bytes.
   auto eights = [](int64_t a) { return a % 8 == 0; };
   auto tma = [&](int64_t token, int64_t head) {
-    return (c->k_rows <= 1 || (token > 0 && eights(token))) && (c->n_kv_heads <= 1 || (head > 0 && eights(head)));
+    return (c->k_rows <= 1 || (token >= c->head_dim && eights(token))) && (c->n_kv_heads <= 1 || (head >= c->head_dim && eights(head)));
   };
   const bool tc = tc_types(c) && c->k_rows > 0 && !low(q, 15u) && !low(k, 15u) && !low(v, 15u) && !low(out, 15u) && eights(c->q_token) &&
                   eights(c->q_head) && eights(c->o_token) && eights(c->o_head) && tma(c->k_token, c->k_head) && tma(c->v_token, c->v_head);

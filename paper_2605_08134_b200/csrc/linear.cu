@@ -415,8 +415,8 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   p.x_row = c->x_row; p.w_row = c->w_row; p.resid_row = c->resid_row; p.y_row = c->y_row;
   p.rows = (int)c->rows; p.n = c->out_features; p.k = c->in_features; p.act = c->activation; p.status = status;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  // a stride that 16-byte accesses can follow (one row has none); rows that repeat (stride 0) stay off the tensor maps
-  auto strides = [&](int64_t rows, int64_t row, int per16) { return rows == 1 || (row > 0 && row % per16 == 0); };
+  // a stride that 16-byte accesses can follow (one row has none); rows that overlap stay off the tensor maps
+  auto strides = [&](int64_t rows, int64_t row, int per16) { return rows == 1 || (row >= c->in_features && row % per16 == 0); };
   cudaError_t e;
   if (c->dtype == DARE_BF16) {
     const bool tc = !low(x, 15u) && !low(w, 15u) && strides(c->rows, c->x_row, 8) && strides(c->out_features, c->w_row, 8);

@@ -6,6 +6,13 @@
 
 namespace dare {
 
+// Rows (stride `row`) of heads (stride `head`) of `width` elements, written by a launch: no two in one place.
+inline bool places_apart(long long rows, long long row, long long heads, long long head, long long width) {
+  if (rows <= 1) return heads <= 1 || head >= width;
+  if (heads <= 1) return row >= width;
+  return head <= row ? head >= width && row >= (heads - 1) * head + width : row >= width && head >= (rows - 1) * row + width;
+}
+
 // rope.cu
 cudaError_t launch_rope_freq_table(const dare_rope_config_t& c, float* table, long long positions, cudaStream_t st);
 cudaError_t launch_rope(const dare_rope_apply_t& c, const void* x, const int* positions, const float* table, void* y, int* status,

@@ -293,8 +293,7 @@ dare_status_t dare_rope(const dare_rope_apply_t* c, const void* x, const int32_t
   if (c->tokens == 0 || c->heads == 0) return DARE_OK;
   if (!x || !y || !table) return DARE_ERR_INVALID_ARG;
   if (c->x_token < 0 || c->x_head < 0 || c->y_token < 0 || c->y_head < 0) return DARE_ERR_SHAPE;
-  // (two tokens or heads of y in one place would be written twice)
-  if ((c->heads > 1 && c->y_head < c->head_dim) || (c->tokens > 1 && c->y_token < c->head_dim)) return DARE_ERR_SHAPE;
+  if (!places_apart(c->tokens, c->y_token, c->heads, c->y_head, c->head_dim)) return DARE_ERR_SHAPE;
   if (x == y && ((c->tokens > 1 && c->x_token != c->y_token) || (c->heads > 1 && c->x_head != c->y_head))) return DARE_ERR_INVALID_ARG;
   const uintptr_t mask = c->dtype == DARE_BF16 ? 1u : 3u;
   if ((reinterpret_cast<uintptr_t>(x) & mask) || (reinterpret_cast<uintptr_t>(y) & mask) || (reinterpret_cast<uintptr_t>(table) & 7u) ||

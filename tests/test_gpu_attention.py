@@ -176,6 +176,11 @@ def test_strides(dare, hd):
     assert torch.equal(out, want)
     dare.attention(q, hm(k), v, qb, kb, causal=True, out=out)
     assert torch.equal(out, want)
+    # keys that overlap: every row of a sliding window over one line
+    line = torch.randn(138 * 8 + 2 * hd, device="cuda").to(BF16)
+    slide = line.as_strided((138, 2, hd), (8, hd, 1))
+    got, lse = dare.attention(q, slide, slide, qb, kb, causal=True, return_lse=True)
+    check(lens, q, slide, slide, qb, kb, got, lse, True, hd ** -0.5, 0.0)
     one_k, one_v = k[:, :1], v[:, :1]
     shared = dare.attention(q, one_k.expand(-1, 2, -1), one_v.expand(-1, 2, -1), qb, kb, causal=True)       # head stride 0
     assert (shared.float() - dare.attention(q, one_k, one_v, qb, kb, causal=True).float()).abs().max().item() <= 2.0 ** -5

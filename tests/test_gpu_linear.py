@@ -116,6 +116,20 @@ def test_not_numbers_stay_in_their_rows_and_columns(dare, dtype, m):
     assert torch.equal(got[got.isinf()].double(), ref[ref.isinf()])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 9, 200])
+def test_rows_that_overlap_and_short_rows(dare, dtype, m):
+    """Inputs whose rows share elements (a sliding window), and rows of one or three elements on the 16-byte grid."""
+    g = torch.Generator(device="cuda").manual_seed(23)
+    line = torch.randn(8 * m + 64, generator=g, device="cuda").to(dtype)
+    x, w = line.as_strided((m, 64), (8, 1)), torch.randn((40, 64), generator=g, device="cuda").to(dtype)
+    check(dare.linear(x, w), x, w, None, None, "none")
+    check(dare.linear(w, line.as_strided((m, 64), (8, 1))), w, x, None, None, "none")
+    for k in (1, 3):
+        x, w = (torch.randn((n, 8), generator=g, device="cuda").to(dtype)[:, :k] for n in (m, 40))
+        check(dare.linear(x, w), x, w, None, None, "none")
+
+
 def test_f32_of_wide_range(dare):
     """The tensor-core form splits operands of any size."""
     g = torch.Generator(device="cuda").manual_seed(17)

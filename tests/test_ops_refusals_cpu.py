@@ -47,7 +47,7 @@ def test_rope(dare):
         assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG, kw
     for kw in (dict(tokens=-1), dict(tokens=(1 << 30) + 1), dict(heads=-1), dict(head_dim=0), dict(rotary_dim=0), dict(rotary_dim=7),
                dict(rotary_dim=66), dict(rotary_dim=258, head_dim=512), dict(table_positions=-1), dict(x_token=-1), dict(y_head=63),
-               dict(y_token=63), dict(x_head=-64)):
+               dict(y_token=63), dict(y_token=127), dict(y_token=64, y_head=255), dict(x_head=-64)):
         assert call(_with(good, **kw)) == dare.ERR_SHAPE, kw
     for kw in (dict(x=None), dict(t=None), dict(y=None)):
         assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
@@ -69,11 +69,11 @@ def test_attention(dare):
 
     assert call(None) == dare.ERR_INVALID_ARG and dare.dare_attention_workspace_bytes(None) == 0
     inf, nan = float("inf"), float("nan")
-    for kw in (dict(struct_size=4), dict(dtype=9), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf)):
+    for kw in (dict(struct_size=4), dict(dtype=9), dict(causal=2), dict(scale=3e38), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf)):
         assert call(_with(good, **kw)) == dare.ERR_INVALID_ARG and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
     for kw in (dict(batch=0), dict(batch=65537), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(head_dim=48),
                dict(q_rows=-1), dict(q_rows=(1 << 24) + 1), dict(k_rows=-1), dict(k_rows=(1 << 30) + 1), dict(k_token=-1), dict(v_head=1 << 38),
-               dict(o_head=127), dict(o_token=127), dict(q_rows=1 << 24, n_heads=128)):
+               dict(o_head=127), dict(o_token=127), dict(o_token=1023), dict(o_token=128, o_head=1024), dict(q_rows=1 << 24, n_heads=128)):
         assert call(_with(good, **kw)) == dare.ERR_SHAPE and dare.dare_attention_workspace_bytes(_with(good, **kw)) == 0, kw
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(qb=None), dict(kb=None), dict(out=None), dict(work=None)):
         assert call(good, **kw) == dare.ERR_INVALID_ARG, kw
