@@ -93,19 +93,32 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
     // (0.75 with few rows) over all SMs, five such for a tile itself, and 13 with the merge.  Tiles / shares in us, heads of 128, 32
     // query and 8 key heads: a prompt of 300 tokens 12.4 / 18.0, 4000 148 / 167, four of up to 1500 81 / 102; 4 and 1 heads: 4000
     // tokens 62 / 44; two blocks of 256 tokens over 8192 keys 124 / 78, four of 512 151 / 173, one token over 4000 keys 42 / 17, four
-    // over 200 8.4 / 11.  Of 64 such shapes (heads of 64 too) the rule takes the slower form, by more than 5 %, in six, by 33 % at most.
+    // over 200 8.4 / 11.  Of 64 such shapes (heads of 64 too) the rule takes the slower form, by more than 5 %, in six, by 33 % at most.  Each CTA of the first looks its
+    // pair up among the sequences' lengths, the shares twice a launch: 256 prompts of up to 200 tokens, 8 and 8 heads, 163 / 161 us,
+    // 1024 1048 / 607.
     const float keys = (float)(c->k_rows / c->batch) / 128.f + 1.f;
     const int64_t rows_each = all / c->batch;
     const float ctas = (float)((all / 256 > c->batch ? all / 256 : c->batch) * c->n_kv_heads);
     const float pairs = (float)((all / 128 > c->batch ? all / 128 : c->batch) * c->n_kv_heads);
-    const float tiles_us = (6.f + keys * (rows_each > 128 ? 2.f : 1.2f)) * fmaxf(1.f, ctas / (float)kSms);
+    const float look_up = 0.012f * (float)c->batch;
+    const float tiles_us = (6.f + look_up + keys * (rows_each > 128 ? 2.f : 1.2f)) * fmaxf(1.f, ctas / (float)kSms);
     const float shares_us = 13.f + pairs * (keys + 5.f) * (rows_each > 64 ? 1.1f : 0.75f) / (float)kSms;
-    const bool tiles = (rows_each > 128 && ctas >= (float)kSms) || tiles_us <= shares_us;
+    const bool tiles = (rows_each > 128 && ctas >= (float)kSms && c->batch <= 256) || tiles_us <= shares_us;
     e = launch_packed_tc(p, c->head_dim, tiles, st);
     if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);
   } else {
+    // Few keys a sequence: a pair is a unit, a CTA has a pair, and there is nothing to merge.  Shares / pairs, us, heads of 64: 16 heads,
+    // four prompts of 100 tokens 16.0 / 14.2, 6 of 113 16.3 / 14.7, one of 60 10.5 / 8.5; heads of 256, 14 of 18 25.3 / 16.7.  With more
+    // keys it depends on the lengths: 8 heads of 128, one prompt of 700 69 / 104.  (One sequence may hold all the keys: eight units.)
+    const int64_t pairs = (all / rows + c->batch) * c->n_kv_heads;                  // at most
+    const bool direct = c->k_rows <= (int64_t)(1 << kUnitShift) * (c->batch < 8 ? c->batch : 8) && pairs <= 8 * kSimtCtas;
+    if (direct) {
+      while (((int64_t)1 << p.unit_shift) < 2 * c->k_rows) ++p.unit_shift;           // (twice: a causal tile's last row is past the end)
+      p.pair_cost = 0;
+      p.n_ctas = (int)pairs;
+    }
     e = launch_packed_simt(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
-    if (e == cudaSuccess) e = launch_packed_combine(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
+    if (e == cudaSuccess && !direct) e = launch_packed_combine(p, c->head_dim, rows, c->dtype == DARE_BF16, st);
   }
   if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }
   return DARE_OK;

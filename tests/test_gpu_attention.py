@@ -140,6 +140,19 @@ def test_many_sequences(dare):
     run(dare, [(i % 3, i % 7) for i in range(150)], 2, 2, 32, F32, True, seed=3)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_keys_a_sequence(dare, causal):
+    """On average; one sequence may hold nearly all of them."""
+    run(dare, [(40, 490), (3, 0), (1, 1), (200, 12)], 6, 2, 64, F32, causal, seed=5)
+    run(dare, [(128, 128)], 4, 4, 256, F32, causal, seed=6)
+    run(dare, [(300, 100), (5, 156)], 8, 1, 32, F32, causal, seed=7)
+
+
+def test_many_prompts(dare):
+    """More sequences than the form with 256 rows a CTA is meant for."""
+    run(dare, [(129 + i % 5, 129 + i % 7) for i in range(300)], 4, 2, 128, BF16, True, seed=8)
+
+
 def test_large_scores(dare):
     """Scores of some hundreds: the weights of all but a few keys vanish, the maximum moves often."""
     run(dare, [(200, 900), (1, 700)], 8, 2, 128, BF16, False, seed=4, std=4.0)
