@@ -451,7 +451,7 @@ def rope(x, table, positions=None, layout=ROPE_LAYOUT["half"], transpose=False, 
     xt, xh, xe = x.stride()
     rows, pairs, two = table.shape
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        out = torch.empty(tokens, heads, hd, dtype=x.dtype, device=x.device)
         yt, yh, ye = heads * hd, hd, 1
     else:
         yt, yh, ye = out.stride()
@@ -493,7 +493,7 @@ def linear(x, w, bias=None, act=ACT["none"], resid=None, out=None, status=None):
     m = x2.shape[0]
     shape = (m, n) if flat else shape[:-1] + (n,)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=x.device)
+        out = torch.empty(*shape, dtype=dtype, device=x.device)           # (sizes one by one: a tuple of them costs a microsecond)
     elif out.shape != shape or out.dtype != dtype:
         raise ValueError("out: [..., out_features] of x's type expected")
     y2 = out if flat else out.view(-1, n)
@@ -541,7 +541,7 @@ def attention(q, k, v, q_begin, k_begin, k_len=None, causal=False, scale=None, o
     kt, kh, ke = k.stride()
     vt, vh, ve = v.stride()
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty(rows, heads, hd, dtype=dtype, device=q.device)
         ot, oh, oe = heads * hd, hd, 1
     else:
         ot, oh, oe = out.stride()
@@ -553,7 +553,7 @@ def attention(q, k, v, q_begin, k_begin, k_len=None, causal=False, scale=None, o
                           k_rows, qt, qh, kt, kh, vt, vh, ot, oh)
     nbytes = _fast_attention_bytes(cfg)
     work = torch.empty(nbytes or 16, dtype=torch.uint8, device=q.device)
-    lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device) if return_lse else None
     _call(_fast_attention, "dare_attention", index, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_begin.data_ptr(),
           k_begin.data_ptr(), None if k_len is None else k_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
           work.data_ptr(), nbytes, None if status is None else status.data_ptr())
