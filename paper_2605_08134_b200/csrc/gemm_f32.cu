@@ -79,7 +79,9 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466
 
 // What a launch takes: a projection's parameters (SG_Q, SG_KV, SG_OUT), or those of the stand-alone product (SG_LINEAR): any
 // number of outputs and of k-elements (multiples of 4), strides, and its own tail; rows and columns past the end are read as the
-// last one, k-elements past the end as zeros.
+// last one, k-elements past the end as zeros.  Few tiles: the blocks of 64 k-elements are shared by a cluster of p.splits CTAs
+// (blockIdx.z); each leaves its sums in shared memory and finishes its part of the rows from everybody's, in the order of the
+// k-elements.
 constexpr int SG_LINEAR = 3;
 template <int EPI>
 using Params = typename std::conditional<EPI == SG_LINEAR, LinearParams, SgemmParams>::type;
@@ -108,16 +110,26 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
     K = p.g.d; half = p.g.head_dim >> 1; lh = 31 - __clz(half);
     n_tiles = K / BN;
   }
-  const int KB = LINEAR ? (K + BK - 1) / BK : K / BK;
+  int KB = K / BK, kb0 = 0, splits = 1;        // blocks of this CTA, the first of them
+  if constexpr (LINEAR) {
+    const int all = (K + BK - 1) / BK;
+    splits = p.splits;
+    kb0 = splits > 1 ? (int)blockIdx.z * all / splits : 0;
+    KB = splits > 1 ? ((int)blockIdx.z + 1) * all / splits - kb0 : all;
+  }
   const bool second = EPI == SG_KV && (int)blockIdx.x >= n_tiles;
   const int pair0 = ((int)blockIdx.x - (second ? n_tiles : 0)) * (BN / 2);
   const float* w;
   if constexpr (LINEAR) w = reinterpret_cast<const float*>(p.w);
   else w = reinterpret_cast<const float*>(second ? p.w1 : p.w0);
   auto column = [&](int pair) { return (pair >> lh) * (2 * half) + (pair & (half - 1)); };
-  const int m0 = (int)(blockIdx.z * gridDim.y + blockIdx.y) * BM;
+  int rows_of_tile = BM, a_chunks = BM / ROWS;   // rows this CTA owns; chunk indexes of A that hold any
+  if constexpr (LINEAR) rows_of_tile = p.tile_rows;
+  const int m0 = (int)((splits > 1 ? 0u : blockIdx.z * gridDim.y) + blockIdx.y) * rows_of_tile;
   if constexpr (LINEAR) {
     if (m0 >= p.rows) return;                    // (the grid's last rows)
+    rows_of_tile = min(rows_of_tile, p.rows - m0);
+    a_chunks = (rows_of_tile + ROWS - 1) / ROWS;
   } else {
     // (row tiles past the first of a gathered launch are usually empty: they look at the count first)
     if (p.count != nullptr && m0 > 0) {
@@ -145,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
     for (int i = 0; i < W_CHUNKS; ++i) {
       const int row = row_of + ROWS * i;
       if constexpr (LINEAR) {
-        src[i] = w + (long long)min(2 * pair0 + row, p.n - 1) * p.w_row + kc;
+        src[i] = w + (long long)min(2 * pair0 + row, p.n - 1) * p.w_row + kb0 * BK + kc;
       } else {
         src[i] = w + (size_t)(column(pair0 + (row & 31)) + (row >> 5) * half) * K + kc;
         v0[i] = load_now(src[i]);
@@ -173,28 +185,32 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
   if (active && splitter) {
 #pragma unroll
     for (int i = W_CHUNKS; i < CHUNKS; ++i) {
-      if constexpr (LINEAR) src[i] = reinterpret_cast<const float*>(p.x) + (long long)min(m0 + row_of + ROWS * i - BN, p.rows - 1) * p.x_row + kc;
+      if constexpr (LINEAR) src[i] = reinterpret_cast<const float*>(p.x) + (long long)min(m0 + row_of + ROWS * i - BN, p.rows - 1) * p.x_row + kb0 * BK + kc;
       else src[i] = reinterpret_cast<const float*>(p.a) + s_row[row_of + ROWS * i - BN] * K + kc;
       if constexpr (!LINEAR) v0[i] = load_now(src[i]);
     }
     if constexpr (LINEAR) {
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) v0[i] = kc < K ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < CHUNKS; ++i)
+        if (i - W_CHUNKS < a_chunks) v0[i] = kb0 * BK + kc < K ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    int k_at = 0;                                // (SG_LINEAR: k-element src stands at, less kc)
+    // (a row of A that nobody owns may hold anything: it counts for its own outputs only)
+    auto live = [&](int i) { return !LINEAR || i < W_CHUNKS || i - W_CHUNKS < a_chunks; };
+    int k_at = kb0 * BK;                                // (SG_LINEAR: k-element src stands at, less kc)
     // Even blocks come into registers, odd ones into a slot of shared memory (a thread's own chunks: nobody else waits for
     // them), the next on its way while one is split.
     auto fetch = [&]() {
       const bool there = !LINEAR || k_at + kc < K;
 #pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) v0[i] = there ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < CHUNKS; ++i)
+        if (live(i)) v0[i] = there ? load_now(src[i]) : make_float4(0.f, 0.f, 0.f, 0.f);
     };
     float* slot = reinterpret_cast<float*>(smem + SLOT_OFFSET) + st_id * 4;
     auto fetch_slot = [&]() {
       const bool there = !LINEAR || k_at + BK + kc < K;      // (else zeros; the address is valid all the same)
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
-        cp_async_16(smem_u32(slot + i * (kSplitters * 4)), there ? src[i] + BK : src[i] - (LINEAR ? k_at + kc : 0), there ? 16u : 0u);
+        if (live(i)) cp_async_16(smem_u32(slot + i * (kSplitters * 4)), there ? src[i] + BK : src[i] - (LINEAR ? k_at + kc : 0), there ? 16u : 0u);
         src[i] += 2 * BK;                        // (the next even block)
       }
       if (LINEAR) k_at += 2 * BK;
@@ -218,6 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
       const uint32_t stage = thread_at + (uint32_t)(s * STAGE_BYTES);
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
+        if (!live(i)) break;
         const uint32_t dst = stage + (uint32_t)(i < W_CHUNKS ? W_OFFSET + ROWS * i * 128 : (ROWS * i - BN) * 128);
         constexpr uint32_t kPart[2] = {A_PART, W_PART};
         const uint32_t part_bytes = kPart[i < W_CHUNKS ? 1 : 0];
@@ -290,6 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
     for (int kb = 0; kb < KB; ++kb) {
       mbar_wait(acc_full, kb & 1, p.status);
       tc_fence_after();
+      if (LINEAR && warp * 32 >= rows_of_tile) {             // (rows that nobody owns)
+        if (lane == 0) mbar_arrive(acc_empty);
+        continue;
+      }
 #pragma unroll
       for (int c = 0; c < BN; c += 8) {
         float v[HH][8];
@@ -347,10 +368,21 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
     float bv[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) bv[i] = bias && c[i] < p.n ? bias[c[i]] : 0.f;
-    __syncthreads();
-    for (int r = warp; r < BM && m0 + r < p.rows; r += kThreads / 32) {
+    const int share = p.tile_rows / splits, r0 = splits > 1 ? (int)blockIdx.z * share : 0;
+    if (splits > 1) cluster_sync_all();
+    else __syncthreads();
+    for (int r = r0 + warp; r < r0 + share && r < rows_of_tile; r += kThreads / 32) {
       const long long row = m0 + r;
       float v[2] = {tile[r * TILE_PITCH + lane], tile[r * TILE_PITCH + 32 + lane]};
+      if (splits > 1) {
+        const uint32_t at = smem_u32(tile + r * TILE_PITCH + lane);
+        v[0] = v[1] = 0.f;
+        for (int s = 0; s < splits; ++s) {
+          const uint32_t from = map_to_cta(at, (uint32_t)s);
+          v[0] += __uint_as_float(ld_cluster_u32(from));
+          v[1] += __uint_as_float(ld_cluster_u32(from + 128));
+        }
+      }
       if (!finite(v[0]) || !finite(v[1])) {
         const int last = p.n - 1;
         const float2 ab = plain_dots(reinterpret_cast<const float*>(p.x) + row * p.x_row, w + (long long)min(c[0], last) * p.w_row,
@@ -368,6 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
           reinterpret_cast<float*>(p.y)[row * p.y_row + c[i]] = v[i];
         }
     }
+    if (splits > 1) cluster_sync_all();          // nobody leaves while its sums are read
   } else if (active) {
     // ---- the projection's own tail: a warp a row, lane <-> rotary pair, the table reads of four rows in flight together
     constexpr int NW = kThreads / 32, RB = 5;    // rows warp, warp + 13, ...: two batches of five
@@ -453,9 +486,10 @@ static cudaError_t launch_as(const SgemmParams& p, cudaStream_t st) {
 cudaError_t launch_linear_f32(const LinearParams& p, cudaStream_t st) {
   static std::atomic<unsigned long long> attr_done{0};
   if (cudaError_t e = ensure_dyn_smem(gemm_f32_kernel<SG_LINEAR>, SMEM_TOTAL, attr_done); e != cudaSuccess) return e;
-  const int row_tiles = (p.rows + BM - 1) / BM, nz = (row_tiles + 65534) / 65535;
-  return launch_pdl(gemm_f32_kernel<SG_LINEAR>, dim3((p.n + BN - 1) / BN, (row_tiles + nz - 1) / nz, nz), dim3(kThreads), SMEM_TOTAL, st, 1,
-                    p);
+  const int row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows, nz = (row_tiles + 65534) / 65535;
+  const int z = p.splits > 1 ? p.splits : nz;    // (splits: few tiles)
+  return launch_pdl(gemm_f32_kernel<SG_LINEAR>, dim3((p.n + BN - 1) / BN, (row_tiles + nz - 1) / nz, z), dim3(kThreads), SMEM_TOTAL, st,
+                    p.splits, p);
 }
 cudaError_t launch_gemm_f32(int epi, const SgemmParams& p, cudaStream_t st) {
   if (p.rows <= 0) return cudaSuccess;

@@ -424,11 +424,25 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   } else {
     const bool aligned = !low(x, 15u) && !low(w, 15u) && c->in_features % 4 == 0 && strides(c->rows, c->x_row, 4) &&
                          strides(c->out_features, c->w_row, 4);
-    // On the tensor cores a tile of 128 rows x 64 outputs takes 4.5 us and 1.1 us a block of 64 k-elements; on the CUDA cores an SM
-    // does about 50 multiply-adds a cycle and a launch takes 6 us at least.
-    const int64_t tiles = (c->rows + 127) / 128 * ((c->out_features + 63) / 64);
-    const float there = (float)((tiles + kSms - 1) / kSms) * (4.5f + 1.1f * (float)((c->in_features + 63) / 64)) + 2.f;
-    const float here = 6.f + (float)((c->rows + 31) / 32 * 32) * (float)c->out_features * (float)c->in_features / (50.f * 1900.f * (float)kSms);
+    // What each takes, us.  Tensor cores: tiles of up to 128 rows x 64 outputs, one an SM at a time, a block of 64 k-elements 0.62 and
+    // 0.0041 a row, shared by a cluster of up to eight (of which kClusters fit beside one another).  601 x 1024 x 1000, 128 rows a tile
+    // 24.4, 80 rows 21.3, 64 34.4; 128 x 8192 x 1000: one CTA a tile 148, four 42, eight 48, four and 64 rows 34.5; 64 x 4096 x 4096 60.4,
+    // two 34.7.  CUDA cores: an SM does about 50 multiply-adds a cycle and a launch takes 6 at least; few rows 1.5 times that: 8 x 2048
+    // x 2048 9.7 (tensor cores 11.2), 16 x 4096 x 4096 30.6 (29.3), 64 77.
+    constexpr int kClusters[4] = {kSms, 72, 32, 14};
+    const int blocks = (c->in_features + 63) / 64, all_rows = (int)((c->rows + 15) / 16) * 16;
+    float there = 1e30f;
+    for (int rows = all_rows < 128 ? all_rows : 128; rows >= 16; rows -= 16) {
+      const int64_t tiles = (c->rows + rows - 1) / rows * ((c->out_features + 63) / 64);
+      for (int i = 0; i < 4 && 1 << i <= blocks; ++i) {
+        const float block = fmaxf(0.72f, 0.62f + 0.0041f * (float)rows);
+        const float us = 1.2f + (float)((tiles + kClusters[i] - 1) / kClusters[i]) *
+                                    ((i ? 5.5f : 4.3f) + block * (float)((blocks + (1 << i) - 1) >> i));
+        if (us < there) { there = us; p.splits = 1 << i; p.tile_rows = rows; }
+      }
+    }
+    const int64_t simt_rows = c->rows <= 8 ? 12 : (c->rows <= 16 ? 24 : (c->rows + 31) / 32 * 32);
+    const float here = 6.f + (float)simt_rows * (float)c->out_features * (float)c->in_features / (50.f * 1900.f * (float)kSms);
     e = aligned && p.rows > 4 && there < here ? launch_linear_f32(p, st) : launch_linear_simt(p, false, st);
   }
   if (e != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }

@@ -13,6 +13,8 @@ struct LinearParams {
   void* y;
   long long x_row, w_row, resid_row, y_row;
   int rows, n, k, act;
+  int tile_rows;             // rows of a tile there: a multiple of 16, at most 128
+  int splits;                // float32 on the tensor cores: CTAs that share a tile's k-elements (1, 2, 4 or 8)
   int* status;
 };
 

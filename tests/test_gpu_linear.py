@@ -130,6 +130,22 @@ def test_rows_that_overlap_and_short_rows(dare, dtype, m):
         check(dare.linear(x, w), x, w, None, None, "none")
 
 
+@pytest.mark.parametrize("m,k,n", [(20, 2048, 2048), (128, 8192, 200), (300, 4096, 1024), (601, 1024, 1000), (48, 4164, 130), (33, 516, 65),
+                                   (90, 200, 64), (16, 12288, 64), (17, 2052, 500)])
+def test_f32_few_tiles(dare, m, k, n):
+    """Tiles of fewer rows, k-elements shared by several CTAs; with what is no number in one CTA's part."""
+    x, w, b, r = make(m, k, n, F32, m + n)
+    y = dare.linear(x, w, bias=b, resid=r, act=dare.ACT["silu"])
+    check(y, x, w, b, r, "silu")
+    assert torch.equal(dare.linear(x, w, bias=b, resid=r, act=dare.ACT["silu"]), y)
+    plain = dare.linear(x, w)
+    x[m - 1, k - 1], w[n - 1, 0], x[0, k // 2] = float("inf"), float("nan"), 3e38
+    got, ref = dare.linear(x, w), x.double() @ w.double().T
+    assert torch.equal(got[1:m - 1, :n - 1], plain[1:m - 1, :n - 1]) and bool(got[:, n - 1].isnan().all())
+    assert bool(got[m - 1, :n - 1].isinf().all()) and torch.equal(got[m - 1, :n - 1].sign().double(), ref[m - 1, :n - 1].sign())
+    check(got[:1, :n - 1], x[:1], w[:n - 1], None, None, "none")
+
+
 def test_f32_of_wide_range(dare):
     """The tensor-core form splits operands of any size."""
     g = torch.Generator(device="cuda").manual_seed(17)
