@@ -387,9 +387,12 @@ cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, cudaStream_t st
 using namespace dare;
 
 namespace {
-// bf16: up to two rows, and up to four of a small W, go to the CUDA cores: four rows of 4096 x 6144 take 18.8 us there and 16 on the
-// tensor cores, of 4096 x 4096 12 and 14, one row of 1024 x 1000 2.0 and 5.
-bool rows_on_cuda_cores(const LinearParams& p) { return p.rows <= 2 || (p.rows <= 4 && (long long)p.n * p.k <= 20 << 20); }
+// bf16, up to four rows, of a W that is not large: CUDA cores / tensor cores, us, one row of 1024 x 1000 2.2 / 3.7, 8192 x 1024 5.1 / 7.8
+// (four 6.7 / 7.8), 4096 x 4096 8.7 / 9.9 (two 9.8 / 9.8, three 11.5 / 9.9), 4096 x 6144 13.0 / 12.1, 4096 x 12288 25.9 / 18.7.
+bool rows_on_cuda_cores(const LinearParams& p) {
+  const long long size = (long long)p.n * p.k;
+  return (p.rows <= 2 && size <= 20 << 20) || (p.rows <= 4 && size <= 12 << 20);
+}
 }  // namespace
 
 extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* x, const void* w, const float* bias, const void* resid,

@@ -1,10 +1,9 @@
 // y = act(x W^T + bias) + resid in bf16 on tcgen05 tensor cores, any number of rows and outputs (dare_ops.h).
 // Persistent: a CTA (or a pair of CTAs sharing M = 256 MMAs, cta_group::2) walks output tiles of 128 (256) rows x `width` columns, the
 // finishing pass of a tile running beside the next one's main loop.  The width is not fixed: it is what the launch rule below
-// finds cheapest, a multiple of 16 up to 256.  With few rows the launch is a stream of W and the width is the outputs over the SMs,
-// so that every SM pulls its share at the same time and no reduction has to be split; only the rows there are come into shared
-// memory then (the MMA's other rows read whatever follows, and nobody reads their results), which leaves up to 12 stages of W on
-// their way.
+// finds cheapest, a multiple of 16 up to 256; where there are few tiles, the rule may share a tile's k-elements between CTAs (the
+// second kernel).  Of few rows only those there are come into shared memory (the MMA's other rows read whatever follows, and nobody
+// reads their results), which leaves up to 12 stages of W on their way.
 //   warp 0     TMA producer: rows of x and of W, 128 k-elements a stage in two boxes of 64 columns each (256 bytes of a row of W come
 //              from one place of the HBM at a time); rows, columns and k-elements past the end are zeros
 //   warp 1     MMA issuer (of a pair: the even CTA's), two accumulators of up to 256 columns of tensor memory in turn
@@ -278,6 +277,156 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
   }
 }
 
+// ------------------------------------------------------------------------------------------------ few tiles
+// A tile's k-blocks shared by a cluster of S CTAs (blockIdx.z), one tile a cluster: tiles stay wide (an SM brings in 128 rows of x for a
+// tile however narrow it is) and every SM still has work.  Each CTA leaves its sums in shared memory, over the ring, and finishes its
+// part of the tile from everybody's, in the order of the k-elements.  Warps 0 and 1 as above, all warps finish.
+template <int S>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const LinearParams p,
+                    const TileWalk t) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + BAR_OFFSET);
+  uint64_t* empty_bar = full_bar + kMaxStages;
+  uint64_t* acc_full = empty_bar + kMaxStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 4);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const int x_bytes = t.x_rows * BK * 2, w_bytes = t.width * BK * 2, stage_bytes = x_bytes + w_bytes;
+  const int stages = min(kMaxStages, kRing / stage_bytes), all = (p.k + BK - 1) / BK, k16 = (p.k + 15) / 16 * 16;
+  const int z = (int)blockIdx.z, kb0 = z * all / S, kb1 = (z + 1) * all / S;
+  const int n0 = (int)blockIdx.x * t.width, m0 = (int)blockIdx.y * BM;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+    mbar_init(acc_full, 1);
+    fence_mbar_init();
+    prefetch_tmap(&tm_x);
+    prefetch_tmap(&tm_w);
+  }
+  if (warp == 1) { tmem_alloc(tmem_slot, 256); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == 0) {
+    for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+      const int s = it % stages;
+      mbar_wait(&empty_bar[s], ((it / stages) & 1) ^ 1, p.status);
+      if (elect_one()) {
+        uint8_t* dst = smem + s * stage_bytes;
+        mbar_arrive_expect_tx(&full_bar[s], (uint32_t)stage_bytes);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k0 = kb * BK + h * 64;
+          tma_load_2d(dst + h * (x_bytes / 2), &tm_x, k0, m0, &full_bar[s]);
+          tma_load_2d(dst + x_bytes + h * (w_bytes / 2), &tm_w, k0, n0, &full_bar[s]);
+        }
+      }
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = idesc_bf16(BM, t.width);
+    for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+      const int s = it % stages;
+      mbar_poll(&full_bar[s], (it / stages) & 1, p.status);
+      tc_fence_after();
+      if (elect_one()) {
+        const uint32_t at = smem_u32(smem + s * stage_bytes);
+        const uint64_t a = smem_desc_k_sw128(at), b = smem_desc_k_sw128(at + x_bytes);
+        const int steps = min(BK, k16 - kb * BK) / 16;
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) {
+          if (k >= steps) break;
+          umma_ss(tmem_base, a + (k >> 2) * (uint32_t)(x_bytes >> 5) + 2 * (k & 3), b + (k >> 2) * (uint32_t)(w_bytes >> 5) + 2 * (k & 3), idesc,
+                  (it | k) != 0 ? 1u : 0u);
+        }
+        umma_commit(&empty_bar[s]);
+        if (kb == kb1 - 1) umma_commit(acc_full);
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  // ---- tensor memory -> shared memory (idle: every MMA is complete, so every load is), thread <-> row
+  float* tile = reinterpret_cast<float*>(smem);
+  const int pitch = t.width + 4, rows = min(BM, p.rows - m0);
+  if (warp >= 2) {
+    const int q = warp & 3, sub = (warp - 2) >> 2;
+    mbar_wait(acc_full, 0, p.status);
+    tc_fence_after();
+    if (q * 32 < rows) {
+      float* dst = tile + (q * 32 + lane) * pitch;
+#pragma unroll 2
+      for (int c = sub * 16; c < t.width; c += 32) {
+        float v[16];
+        tmem_ld_32x16_nowait(tmem_base + ((uint32_t)(q * 32) << 16) + c, v);
+        tmem_ld_wait();
+        if (q * 32 + lane < rows) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dst + c + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  cluster_sync_all();
+  if (warp == 1) tmem_dealloc(tmem_base, 256);
+  // ---- eight columns a thread
+  const int eights = t.width / 8, items = rows * eights, first = z * items / S, last = (z + 1) * items / S;
+  for (int e = first + (int)threadIdx.x; e < last; e += kThreads) {
+    const int r = e / eights, c = (e - r * eights) * 8;
+    const uint32_t at = smem_u32(tile + r * pitch + c);
+    float4 a[S], b[S];                // (all of them on their way at once)
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const uint32_t from = map_to_cta(at, (uint32_t)s);
+      a[s] = ld_cluster_f4(from);
+      b[s] = ld_cluster_f4(from + 16);
+    }
+    float v[8] = {};
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      v[0] += a[s].x; v[1] += a[s].y; v[2] += a[s].z; v[3] += a[s].w;
+      v[4] += b[s].x; v[5] += b[s].y; v[6] += b[s].z; v[7] += b[s].w;
+    }
+    const int cols = p.n - (n0 + c);
+    if (cols <= 0) continue;
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < cols) v[i] += __ldg(p.bias + n0 + c + i);
+    }
+    activate<true>(v, p.act);
+    const long long row = m0 + r;
+    __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + row * p.y_row + n0 + c;
+    const __nv_bfloat16* resid = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + row * p.resid_row + n0 + c : nullptr;
+    if (t.wide_y && cols >= 8) {
+      if (resid) {
+        const uint4 raw = *reinterpret_cast<const uint4*>(resid);
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = __bfloat1622float2(h[i]);
+          v[2 * i] += f.x;
+          v[2 * i + 1] += f.y;
+        }
+      }
+      *reinterpret_cast<uint4*>(y) = pack8_bf16(v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < cols) y[i] = __float2bfloat16_rn(resid ? v[i] + __bfloat162float(resid[i]) : v[i]);
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();                // nobody leaves while its sums are read
+}
+
 // Tile width and form: waves of tiles times what a k-block takes an SM (the tensor pipe's cycles, or the operand bytes
 // at 64 a cycle), plus the finishing pass of the last tile.  us by width, p: pairs, the pick in brackets:
 //   37 rows of 4096 x 12288   48 27.7, 64 28.5, [96 21.3], 128 21.9, 160 23.6, 192 24.2, 256 32.5
@@ -286,24 +435,52 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
 //   512 of 4096 x 4096        96 30.7, 128 19.2, p96 25.3, [p128 16.9], p160 21.2, p256 25.0
 //   2048 of 4096 x 4096       128 64.5, 256 59.6, p128 53.6, p160 52.1, p224 59.0, [p256 49.2]
 // At the ten sizes timed (8 to 2048 rows) the pick was the fastest or within 0.4 us of it.
-struct Form { int pair, width; };
+struct Form { int pair, width, splits; };
 Form pick_form(int rows, int n, int k) {
   const int m_tiles = (rows + BM - 1) / BM, KB = (k + BK - 1) / BK, x_rows = rows < BM ? (rows + 7) / 8 * 8 : BM;
-  Form best{0, 16};
-  float least = 1e30f;
+  Form best{0, 16, 1};
+  float least = 1e30f, best_block = 0.f;
   for (int pair = 0; pair <= (m_tiles > 1 ? 1 : 0); ++pair)
     for (int width = pair ? 32 : 16; width <= 256; width += pair ? 32 : 16) {
       const int units = (n + width - 1) / width * (pair ? (m_tiles + 1) / 2 : m_tiles), slots = pair ? kSms / 2 : kSms;
       const float waves = (float)((units + slots - 1) / slots);
       const float mma = 8.f * fmaxf(48.f, 129.f * (float)width / 256.f);
       const float feed = (float)(x_rows + (pair ? width / 2 : width)) * (float)(BK * 2) / 64.f;
-      const float cycles = waves * (float)KB * fmaxf(mma, feed) + 6.f * (float)width;
-      if (cycles < least) { least = cycles; best = Form{pair, width}; }
+      const float block = waves * fmaxf(mma, feed), cycles = block * (float)KB + 6.f * (float)width;
+      if (cycles < least) { least = cycles; best = Form{pair, width, 1}; best_block = fmaxf(block, 590.f * waves); }
+    }
+  // Shared k-elements: what that takes in us, the larger of the SMs' and the memory's time and a fifth of the other, against the same for
+  // the tile found above (where a block of k-elements takes 590 cycles at least).  A tile's own time is 3.2 us and 0.2 us a 1000
+  // elements of it.  Whole tiles / two / four / eight CTAs a tile, the pick in brackets:
+  //   8 rows of 12288 x 4096   35.7 / 24.1 / [19.8] / 24.8       64 of 8192 x 1000   25.2 / 14.9 / 10.1 / [9.2]
+  //   100 of 10000 x 200       30.2 / 17.3 / 10.3 / [7.6]        128 of 12288 x 512  36.8 / 20.8 / 12.9 / [10.3]
+  //   512 of 8192 x 1024       22.8 / 18.0 / [15.9] / 38.2       256 of 4096 x 4096  [15.9] / 14.5 / 20.7
+  //   1024 of 1024 x 1024      [7.3] / 8.5 / 14.1                16 of 4096 x 6144   16.6 / 12.5 / [12.5] / 18.0
+  // Of 22 such sizes the pick was at most 10 % behind the fastest.  (More tiles than clusters that fit beside one another: two waves.)
+  if ((long long)m_tiles * ((n + 255) / 256) > 2 * kSms) return best;
+  constexpr int kClusters[3] = {72, 32, 14};
+  const float memory = 2.f * ((float)rows * (float)k + (float)n * (float)k + (float)rows * (float)n) / 6.5e6f;
+  auto both = [](float a, float b) { return fmaxf(a, b) + 0.2f * fminf(a, b); };
+  float least_us = both((best_block * (float)KB + 6.f * (float)best.width) / 1900.f + 4.f, memory + 4.f);
+  for (int i = 0; i < 3 && 2 << i <= KB; ++i)
+    for (int width = 16; width <= 256 && width < n + 16; width += 16) {
+      const int tiles = m_tiles * ((n + width - 1) / width);
+      const float block = fmaxf(590.f, fmaxf(8.f * 129.f * (float)width / 256.f, (float)(x_rows + width) * (float)(BK * 2) / 64.f)) / 1900.f;
+      const float own = 0.0002f * (float)(x_rows * width);
+      const float us = both((float)((tiles + kClusters[i] - 1) / kClusters[i]) * ((float)((KB + (2 << i) - 1) >> (i + 1)) * block + 3.2f + own),
+                            memory + 3.2f + 0.5f * own);
+      if (us < least_us) { least_us = us; best = Form{0, width, 2 << i}; }
     }
   return best;
 }
 }  // namespace
 
+template <int S>
+static cudaError_t launch_split(const CUtensorMap& mx, const CUtensorMap& mw, const LinearParams& p, const TileWalk& t, cudaStream_t st) {
+  static std::atomic<unsigned long long> done{0};
+  if (cudaError_t e = ensure_dyn_smem(linear_split_kernel<S>, SMEM_TOTAL, done); e != cudaSuccess) return e;
+  return launch_pdl(linear_split_kernel<S>, dim3((unsigned)t.n_tiles, (unsigned)t.m_units, S), dim3(kThreads), SMEM_TOTAL, st, S, mx, mw, p, t);
+}
 cudaError_t launch_linear_tc(const LinearParams& p, cudaStream_t st) {
   const Form f = pick_form(p.rows, p.n, p.k);
   const int m_tiles = (p.rows + BM - 1) / BM;
@@ -323,6 +500,9 @@ cudaError_t launch_linear_tc(const LinearParams& p, cudaStream_t st) {
   if (!make_map_strided(&mx, p.x, p.rows, p.k, p.rows == 1 ? k8 : p.x_row, t.x_rows) ||
       !make_map_strided(&mw, p.w, p.n, p.k, p.n == 1 ? k8 : p.w_row, f.pair ? f.width / 2 : f.width))
     return cudaErrorInvalidValue;
+  if (f.splits == 2) return launch_split<2>(mx, mw, p, t, st);
+  if (f.splits == 4) return launch_split<4>(mx, mw, p, t, st);
+  if (f.splits == 8) return launch_split<8>(mx, mw, p, t, st);
   const long long units = (long long)t.n_tiles * t.m_units;
   static std::atomic<unsigned long long> done1{0}, done2{0};
   if (f.pair) {

@@ -146,6 +146,25 @@ def test_f32_few_tiles(dare, m, k, n):
     check(got[:1, :n - 1], x[:1], w[:n - 1], None, None, "none")
 
 
+@pytest.mark.parametrize("m,k,n", [(1, 4096, 6144), (3, 4096, 4096), (8, 12288, 4096), (20, 8200, 1000), (100, 10000, 200), (64, 1032, 1024),
+                                   (130, 520, 530), (300, 4096, 1023), (257, 2048, 256), (512, 8192, 1024), (33, 2056, 17)])
+def test_bf16_few_tiles(dare, m, k, n):
+    """k-elements shared by several CTAs; y on and off the 16-byte grid, on top of the residual; what is no number in one CTA's part."""
+    x, w, b, r = make(m, k, n, BF16, m + n)
+    y = dare.linear(x, w, bias=b, resid=r, act=dare.ACT["silu"])
+    check(y, x, w, b, r, "silu")
+    off = torch.full((m, n + 3), 7.0, dtype=BF16, device="cuda")
+    off[:, :n] = r
+    dare.linear(x, w, bias=b, resid=off[:, :n], act=dare.ACT["silu"], out=off[:, :n])
+    assert torch.equal(off[:, :n], y) and bool((off[:, n:] == 7.0).all())
+    plain = dare.linear(x, w)
+    check(plain, x, w, None, None, "none")
+    x[m - 1, k - 1], w[n - 1, 0] = float("inf"), float("nan")
+    got, ref = dare.linear(x, w), x.double() @ w.double().T
+    assert torch.equal(got[:m - 1, :n - 1], plain[:m - 1, :n - 1]) and bool(got[:, n - 1].isnan().all())
+    assert bool(got[m - 1, :n - 1].isinf().all()) and torch.equal(got[m - 1, :n - 1].sign().double(), ref[m - 1, :n - 1].sign())
+
+
 def test_f32_of_wide_range(dare):
     """The tensor-core form splits operands of any size."""
     g = torch.Generator(device="cuda").manual_seed(17)
