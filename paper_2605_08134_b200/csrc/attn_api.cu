@@ -55,7 +55,7 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   auto low = [](const void* p, uintptr_t mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; };
   const uintptr_t elem = c->dtype == DARE_BF16 ? 1u : 3u;
   if (low(q, elem) || low(k, elem) || low(v, elem) || low(out, elem) || low(q_begin, 3u) || low(k_begin, 3u) || low(k_len, 3u) ||
-      low(lse, 3u) || low(workspace, 15u))
+      low(lse, 3u) || low(workspace, 15u) || low(status, 3u))
     return DARE_ERR_ALIGN;
   if (workspace_bytes < dare_attention_workspace_bytes(c)) return DARE_ERR_WORKSPACE;
   cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -169,8 +169,9 @@ struct Line {
     out->tiles = __shfl_sync(0xffffffffu, tiles, src);
     const unsigned per_head = __shfl_sync(0xffffffffu, head, src);
     const unsigned in_seq = u - base - __shfl_sync(0xffffffffu, inc - head * (unsigned)p.kv_heads, src);
-    out->h = (int)(in_seq / per_head);                                        // head by head
-    const unsigned in_head = in_seq - (unsigned)out->h * per_head;
+    // (head by head; the bound holds by itself unless slices that overlap make the line longer than 32 bits)
+    out->h = min((int)(in_seq / per_head), p.kv_heads - 1);
+    const unsigned in_head = min(in_seq - (unsigned)out->h * per_head, per_head - 1);
     if (!UNITS) {
       out->tile = out->tiles - 1 - (int)in_head;                              // the longest first
       out->units = 1;

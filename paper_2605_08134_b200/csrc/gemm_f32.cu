@@ -400,6 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
           reinterpret_cast<float*>(p.y)[row * p.y_row + c[i]] = v[i];
         }
     }
+    __syncwarp();
     if (splits > 1) cluster_sync_all();          // nobody leaves while its sums are read
   } else if (active) {
     // ---- the projection's own tail: a warp a row, lane <-> rotary pair, the table reads of four rows in flight together

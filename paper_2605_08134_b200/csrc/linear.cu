@@ -411,7 +411,7 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   if (resid == y && c->rows > 1 && c->resid_row != c->y_row) return DARE_ERR_INVALID_ARG;
   auto low = [](const void* p, uintptr_t mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; };
   const uintptr_t elem = c->dtype == DARE_BF16 ? 1u : 3u;
-  if (low(x, elem) || low(w, elem) || low(resid, elem) || low(y, elem) || low(bias, 3u)) return DARE_ERR_ALIGN;
+  if (low(x, elem) || low(w, elem) || low(resid, elem) || low(y, elem) || low(bias, 3u) || low(status, 3u)) return DARE_ERR_ALIGN;
 
   LinearParams p = {};
   p.x = x; p.w = w; p.bias = bias; p.resid = resid; p.y = y;

@@ -297,7 +297,7 @@ dare_status_t dare_rope(const dare_rope_apply_t* c, const void* x, const int32_t
   if (x == y && ((c->tokens > 1 && c->x_token != c->y_token) || (c->heads > 1 && c->x_head != c->y_head))) return DARE_ERR_INVALID_ARG;
   const uintptr_t mask = c->dtype == DARE_BF16 ? 1u : 3u;
   if ((reinterpret_cast<uintptr_t>(x) & mask) || (reinterpret_cast<uintptr_t>(y) & mask) || (reinterpret_cast<uintptr_t>(table) & 7u) ||
-      (reinterpret_cast<uintptr_t>(positions) & 3u))
+      (reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(status) & 3u))
     return DARE_ERR_ALIGN;
   if (launch_rope(*c, x, positions, table, y, status, (cudaStream_t)cuda_stream) != cudaSuccess) { cudaGetLastError(); return DARE_ERR_CUDA; }
   return DARE_OK;

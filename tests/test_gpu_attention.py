@@ -254,6 +254,21 @@ def test_slices_outside_the_arrays(dare, dtype, hd):
         assert torch.allclose(out[keep].float(), want[keep].float(), atol=2.0 ** -6)      # (shares cut elsewhere: other roundings)
 
 
+@pytest.mark.parametrize("dtype,hd,n", [(BF16, 128, 30), (F32, 64, 30), (F32, 64, 1500), (BF16, 64, 1500)])
+def test_slices_that_run_backwards(dare, dtype, hd, n):
+    """Offsets that go back and forth: the slices that run backwards are skipped, and those that then overlap are each right."""
+    q, k, v, qb, kb, _ = make([(70, n)], 4, 2, hd, dtype, 12, tail=2)
+    want = dare.attention(q, k, v, qb, kb)[:70]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    status, out = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full_like(q, 7.0)
+    dare.attention(q, k, v, ints([0, 70] * 40), ints([0] * 79), k_len=ints([n] * 79), out=out, status=status)
+    assert status.item() == dare.ERR_DEVICE_CHECK
+    bad = (out[:70].float() - want.float()).abs() > 2.0 ** -6
+    rows = bad.flatten(1).any(1)
+    assert not bool((rows & (out[:70] != 7.0).flatten(1).all(1)).any())          # (a row may be left out)
+    assert bool((out[70:] == 7.0).all())
+
+
 def test_streams_and_graphs(dare):
     lens = [(1, 3000), (1, 77), (1, 1500), (1, 1)]
     q, k, v, qb, kb, _ = make(lens, 32, 8, 128, BF16, 11, tail=0)

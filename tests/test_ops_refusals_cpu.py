@@ -100,3 +100,13 @@ def test_linear(dare):
     for kw in (dict(x=P + 1), dict(w=Q + 1), dict(y=R + 1), dict(b=S + 2), dict(r=S + 1)):
         assert call(good, **kw) == dare.ERR_ALIGN, kw
     assert call(_with(good, rows=0), x=None) == dare.OK
+
+
+def test_status_off_its_grid(dare):
+    ap = dare.RopeApply(C.sizeof(dare.RopeApply), dare.BF16, 4, 2, 64, 64, 0, 0, 0, 128, 64, 128, 64, 16)
+    assert dare.dare_rope(ap, P, None, Q, R, S + 2) == dare.ERR_ALIGN
+    lc = dare.LinearConfig(C.sizeof(dare.LinearConfig), dare.BF16, 4, 64, 32, 0, 0, 64, 64, 32, 32)
+    assert dare.dare_linear(lc, P, Q, None, None, R, S + 2) == dare.ERR_ALIGN
+    ac = dare.AttentionConfig(C.sizeof(dare.AttentionConfig), dare.BF16, 2, 8, 2, 128, 1, 0.1, 16, 64, 1024, 128, 256, 128, 256, 128, 1024, 128)
+    need = dare.dare_attention_workspace_bytes(ac)
+    assert dare.dare_attention(ac, P, Q, R, S, S + 64, None, 0x50000, None, 0x900000, need, S + 2) == dare.ERR_ALIGN
