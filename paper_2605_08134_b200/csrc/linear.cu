@@ -92,9 +92,16 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
   for (int i = 0; i < MT; ++i) x[i] = reinterpret_cast<const T*>(p.x) + (long long)min(i, p.rows - 1) * p.x_row;
 #pragma unroll
   for (int j = 0; j < kOut; ++j) w[j] = reinterpret_cast<const T*>(p.w) + min(n0 + j, (long long)p.n - 1) * p.w_row;
-  float2 sums[kOut * MT];
+  constexpr int N = kOut * MT, LEFT = N > 32 ? N / 32 : 1;
+  // the output this thread finishes: group of outputs, value of it; its bias and residual come beside the sums
+  const int out = (int)threadIdx.x / N, value = (int)threadIdx.x % N, m = value / kOut;
+  const long long n = ((long long)blockIdx.x * (kWarps / k_warps) + out) * kOut + value % kOut;
+  const bool mine = out < kWarps / k_warps && m < p.rows && n < p.n;
+  const float bias = mine && p.bias ? p.bias[n] : 0.f;
+  const float resid = mine && p.resid ? (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n] : 0.f;
+  float2 sums[N];
 #pragma unroll
-  for (int i = 0; i < kOut * MT; ++i) sums[i] = make_float2(0.f, 0.f);
+  for (int i = 0; i < N; ++i) sums[i] = make_float2(0.f, 0.f);
   auto multiply = [&](const float2 (&a)[VE / 2], const float2 (&b)[VE / 2], int at) {
 #pragma unroll
     for (int e = 0; e < VE / 2; ++e) sums[at] = __ffma2_rn(a[e], b[e], sums[at]);
@@ -150,10 +157,9 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
       }
     }
   }
-  float acc[kOut * MT];
+  float acc[N];
 #pragma unroll
-  for (int i = 0; i < kOut * MT; ++i) acc[i] = sums[i].x + sums[i].y;
-  constexpr int N = kOut * MT, LEFT = N > 32 ? N / 32 : 1;
+  for (int i = 0; i < N; ++i) acc[i] = sums[i].x + sums[i].y;
   int first = 0;
   reduce_lanes<N, 16>(acc, &first);
   // (fewer values than lanes: the lanes with the same ones differ in the low bits, the first of them writes)
@@ -162,17 +168,12 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
     for (int i = 0; i < LEFT; ++i) parts[warp][first + i] = acc[i];
   }
   __syncthreads();
-  const int out = (int)threadIdx.x / N, i = (int)threadIdx.x % N;              // group of outputs, value of it
-  if (out >= kWarps / k_warps) return;
+  if (!mine) return;
   float v[1] = {0.f};
-  for (int s = 0; s < k_warps; ++s) v[0] += parts[out * k_warps + s][i];
-  const int m = i / kOut;
-  const long long n = ((long long)blockIdx.x * (kWarps / k_warps) + out) * kOut + i % kOut;
-  if (m >= p.rows || n >= p.n) return;
-  if (p.bias) v[0] += p.bias[n];
+  for (int s = 0; s < k_warps; ++s) v[0] += parts[out * k_warps + s][value];
+  v[0] += bias;
   activate<sizeof(T) == 2>(v, p.act);
-  if (p.resid) v[0] += (float)reinterpret_cast<const T*>(p.resid)[(long long)m * p.resid_row + n];
-  reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)v[0];
+  reinterpret_cast<T*>(p.y)[(long long)m * p.y_row + n] = (T)(v[0] + resid);
 }
 
 template <typename T, int MT, int VE, bool WIDE>

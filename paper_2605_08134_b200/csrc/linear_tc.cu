@@ -20,7 +20,9 @@ namespace {
 constexpr int BM = 128, BK = 128, kFinish = 8, kThreads = (2 + kFinish) * 32;
 constexpr int kRing = 192 * 1024, kMaxStages = 12;
 constexpr int HALF_X = BM * 128;                           // 128 rows of 64 k-elements, what an MMA reads as its rows of x ...
-constexpr int BAR_OFFSET = kRing + HALF_X;                 // ... from where a stage's begin, however few it has
+constexpr int BIAS_OFFSET = kRing + HALF_X;                // ... from where a stage's begin, however few it has
+constexpr int kBiasCols = 128;                             // a finishing warp's columns of the widest tile
+constexpr int BAR_OFFSET = BIAS_OFFSET + kFinish * kBiasCols * 4;
 constexpr int SMEM_TOTAL = BAR_OFFSET + 512 + 1024;
 static_assert(SMEM_TOTAL <= 227 * 1024 && (2 * kMaxStages + 4) * 8 + 4 <= 512, "shared memory of one CTA");
 constexpr int kGroupBytes = 24 << 20;                      // column tiles are walked in groups of this much of W, as in gemm_persist.cu
@@ -29,7 +31,7 @@ struct TileWalk {
   int width, x_rows;          // columns of a tile; rows of x a stage holds
   int n_tiles, m_units;       // column tiles; row tiles (PAIR: pairs of them)
   int n_group;
-  int wide_y, wide_bias;      // y (and resid) by 16 bytes, bias by 16 bytes
+  int wide_y;                 // y (and resid) by 16 bytes
 };
 
 template <bool PAIR>
@@ -162,65 +164,90 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
       int m0, n0;
       tile_of(u, &m0, &n0);
       const uint32_t buf = tcount & 1;
+      // (the warp's part of the bias while the tile is multiplied: read where it is used, it held every 32 columns up for 0.7 us)
+      const int cols = min(t.width, p.n - n0);
+      float* bias_sh = reinterpret_cast<float*>(smem + BIAS_OFFSET) + (warp - 2) * kBiasCols;
+      if (p.bias) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kBiasCols; i += 32) {
+          const int e = i + lane, run = t.wide_y ? 31 : 15;          // the warps of a quarter take runs of 32 (16) columns in turn
+          const int c = 2 * (e & ~run) + sub * (run + 1) + (e & run);
+          if (c < cols) bias_sh[e] = __ldg(p.bias + n0 + c);
+        }
+        __syncwarp();
+      }
+      uint8_t* stg = smem + kRing + (warp - 2) * 2048;
+      const int pr8 = lane >> 2, unit = lane & 3, rows = p.rows - (m0 + q * 32);
+      const long long piece = (long long)(m0 + q * 32 + pr8);
+      __nv_bfloat16* yp = reinterpret_cast<__nv_bfloat16*>(p.y) + piece * p.y_row + n0 + unit * 8;
+      const __nv_bfloat16* rp = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + piece * p.resid_row + n0 + unit * 8 : nullptr;
+      uint4 rs[4];                   // of 32 rows x 32 columns of resid; the next ones come while these are used
+      auto load_resid = [&](int c) {
+        if (rp == nullptr || !t.wide_y || c + 32 > cols) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i * 8 + pr8 < rows) rs[i] = *reinterpret_cast<const uint4*>(rp + c + i * 8 * p.resid_row);
+      };
+      load_resid(sub * 32);
       mbar_wait(&acc_full[buf], (tcount >> 1) & 1, p.status);
       tc_fence_after();
       const uint32_t t_lane = tmem_base + buf * 256 + ((uint32_t)(q * 32) << 16);
-      const int row = m0 + q * 32 + lane, cols = min(t.width, p.n - n0);
+      const int row = m0 + q * 32 + lane;
       const bool warp_has_rows = m0 + q * 32 < p.rows;
       __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (long long)row * p.y_row + n0;
       const __nv_bfloat16* resid = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + (long long)row * p.resid_row + n0 : nullptr;
       if (warp_has_rows && t.wide_y) {
+        // 32 rows x 32 columns at a time between the threads' rows and whole 64-byte pieces of y and resid, through 2 KB of shared
+        // memory (past the ring; 16-byte units swizzled by row).  Stores straight from the threads' rows touch 32 lines each.
+        auto place = [&](int r, int u) { return reinterpret_cast<uint4*>(stg + r * 64 + ((u ^ ((r >> 1) & 3)) << 4)); };
 #pragma unroll 1
         for (int c = sub * 32; c < cols; c += 64) {
           const bool full = c + 32 <= cols;
           float v[32];
           tmem_ld_32x32_nowait(t_lane + c, v);
-          uint4 rs[4];
-          if (resid && full && row < p.rows) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rs[i] = *reinterpret_cast<const uint4*>(resid + c + 8 * i);
-          }
           tmem_ld_wait();
           if (p.bias) {
-            const float* b = p.bias + n0 + c;
-            if (full && t.wide_bias) {
+            const float4* b = reinterpret_cast<const float4*>(bias_sh + ((c >> 1) & ~31));        // (columns past the end: anything)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float4 f = __ldg(reinterpret_cast<const float4*>(b) + i);
-                v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c + i < cols) v[i] += __ldg(b + i);
+            for (int i = 0; i < 8; ++i) {
+              const float4 f = b[i];
+              v[4 * i] += f.x; v[4 * i + 1] += f.y; v[4 * i + 2] += f.z; v[4 * i + 3] += f.w;
             }
           }
           activate<true>(v, p.act);
-          if (row < p.rows) {
-            if (full) {
-              if (resid) {
+          if (full) {
+            if (resid) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&rs[i]);
+              for (int i = 0; i < 4; ++i) *place(i * 8 + pr8, unit) = rs[i];
+              load_resid(c + 64);
+              __syncwarp();
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const float2 f = __bfloat1622float2(h[e]);
-                    v[8 * i + 2 * e] += f.x;
-                    v[8 * i + 2 * e + 1] += f.y;
-                  }
+              for (int i = 0; i < 4; ++i) {
+                const uint4 raw = *place(lane, i);
+                const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 f = __bfloat1622float2(h[e]);
+                  v[8 * i + 2 * e] += f.x;
+                  v[8 * i + 2 * e + 1] += f.y;
                 }
               }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(y + c)[i] = pack8_bf16(v + 8 * i);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (c + i < cols) {
-                  float o = v[i];
-                  if (resid) o += __bfloat162float(resid[c + i]);
-                  y[c + i] = __float2bfloat16_rn(o);
-                }
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *place(lane, i) = pack8_bf16(v + 8 * i);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (i * 8 + pr8 < rows) *reinterpret_cast<uint4*>(yp + c + i * 8 * p.y_row) = *place(i * 8 + pr8, unit);
+          } else if (row < p.rows) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (c + i < cols) {
+                float o = v[i];
+                if (resid) o += __bfloat162float(resid[c + i]);
+                y[c + i] = __float2bfloat16_rn(o);
+              }
           }
           __syncwarp();
         }
@@ -228,7 +255,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         // Rows of y or resid that are not on the 16-byte grid: 16 columns at a time through 2 KB of shared memory (the rows that the
         // last stage's MMA reads past its own; units of 16 bytes swizzled by row), from where half a warp takes a row: 2-byte
         // stores of 32 rows at a time took as long as the main loop (3080 x 6400 x 1899: 111 us, 64 so).
-        float* stg = reinterpret_cast<float*>(smem + kRing) + (warp - 2) * (32 * 16);
+        float* stg_f = reinterpret_cast<float*>(stg);
         const int lr = lane >> 4, lc = lane & 15;
 #pragma unroll 1
         for (int c = sub * 16; c < cols; c += 32) {
@@ -237,16 +264,15 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<float4*>(stg + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            *reinterpret_cast<float4*>(stg_f + lane * 16 + ((i ^ ((lane >> 1) & 3)) << 2)) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           __syncwarp();
           const bool there = c + lc < cols;
-          const float bias = p.bias && there ? __ldg(p.bias + n0 + c + lc) : 0.f;
-          const int rows = min(32, p.rows - (m0 + q * 32));
+          const float bias = p.bias ? bias_sh[((c >> 1) & ~15) + lc] : 0.f;
           float o[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int r = 2 * i + lr;
-            o[i] = stg[r * 16 + ((((lc >> 2) ^ ((r >> 1) & 3)) << 2) | (lc & 3))] + bias;
+            o[i] = stg_f[r * 16 + ((((lc >> 2) ^ ((r >> 1) & 3)) << 2) | (lc & 3))] + bias;
           }
           activate<true>(o, p.act);
           const long long row0 = m0 + q * 32 + lr;
@@ -311,7 +337,20 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
   const uint32_t tmem_base = *tmem_slot;
   pdl_wait();
   pdl_launch_dependents();
-
+  // What a thread finishes: eight columns of a row at a time.  Bias and residual of its first eight come beside the main loop.
+  const int rows = min(BM, p.rows - m0), eights = t.width / 8, items = rows * eights, first = z * items / S, last = (z + 1) * items / S;
+  float bias[8];
+  uint4 rs;
+  auto fetch = [&](int e) {
+    const int r = e / eights, n = n0 + (e - r * eights) * 8;
+    if (e >= last || n >= p.n) return;
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) bias[i] = __ldg(p.bias + min(n + i, p.n - 1));
+    }
+    if (p.resid && t.wide_y && n + 8 <= p.n)
+      rs = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.resid) + (long long)(m0 + r) * p.resid_row + n);
+  };
   if (warp == 0) {
     for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
       const int s = it % stages;
@@ -351,9 +390,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
     }
   }
   __syncwarp();
+  fetch(first + (int)threadIdx.x);
   // ---- tensor memory -> shared memory (idle: every MMA is complete, so every load is), thread <-> row
   float* tile = reinterpret_cast<float*>(smem);
-  const int pitch = t.width + 4, rows = min(BM, p.rows - m0);
+  const int pitch = t.width + 4;
   if (warp >= 2) {
     const int q = warp & 3, sub = (warp - 2) >> 2;
     mbar_wait(acc_full, 0, p.status);
@@ -377,7 +417,6 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
   cluster_sync_all();
   if (warp == 1) tmem_dealloc(tmem_base, 256);
   // ---- eight columns a thread
-  const int eights = t.width / 8, items = rows * eights, first = z * items / S, last = (z + 1) * items / S;
   for (int e = first + (int)threadIdx.x; e < last; e += kThreads) {
     const int r = e / eights, c = (e - r * eights) * 8;
     const uint32_t at = smem_u32(tile + r * pitch + c);
@@ -396,10 +435,10 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
     }
     const int cols = p.n - (n0 + c);
     if (cols <= 0) continue;
+    if (e != first + (int)threadIdx.x) fetch(e);
     if (p.bias) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < cols) v[i] += __ldg(p.bias + n0 + c + i);
+      for (int i = 0; i < 8; ++i) v[i] += bias[i];
     }
     activate<true>(v, p.act);
     const long long row = m0 + r;
@@ -407,8 +446,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
     const __nv_bfloat16* resid = p.resid ? reinterpret_cast<const __nv_bfloat16*>(p.resid) + row * p.resid_row + n0 + c : nullptr;
     if (t.wide_y && cols >= 8) {
       if (resid) {
-        const uint4 raw = *reinterpret_cast<const uint4*>(resid);
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&raw);
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&rs);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float2 f = __bfloat1622float2(h[i]);
@@ -454,8 +492,8 @@ Form pick_form(int rows, int n, int k) {
   // elements of it.  Whole tiles / two / four / eight CTAs a tile, the pick in brackets:
   //   8 rows of 12288 x 4096   35.7 / 24.1 / [19.8] / 24.8       64 of 8192 x 1000   25.2 / 14.9 / 10.1 / [9.2]
   //   100 of 10000 x 200       30.2 / 17.3 / 10.3 / [7.6]        128 of 12288 x 512  36.8 / 20.8 / 12.9 / [10.3]
-  //   512 of 8192 x 1024       22.8 / 18.0 / [15.9] / 38.2       256 of 4096 x 4096  [15.9] / 14.5 / 20.7
-  //   1024 of 1024 x 1024      [7.3] / 8.5 / 14.1                16 of 4096 x 6144   16.6 / 12.5 / [12.5] / 18.0
+  //   512 of 8192 x 1024       22.8 / 18.0 / [15.9] / 38.2       256 of 4096 x 4096  [14.9] / 14.5 / 20.7
+  //   1024 of 1024 x 1024      [6.6] / 8.5 / 14.1                16 of 4096 x 6144   16.6 / 12.5 / [12.5] / 18.0
   // Of 22 such sizes the pick was at most 10 % behind the fastest.  (More tiles than clusters that fit beside one another: two waves.)
   if ((long long)m_tiles * ((n + 255) / 256) > 2 * kSms) return best;
   constexpr int kClusters[3] = {72, 32, 14};
@@ -493,7 +531,6 @@ cudaError_t launch_linear_tc(const LinearParams& p, cudaStream_t st) {
   t.n_group = (int)(kGroupBytes / tile_bytes > 0 ? kGroupBytes / tile_bytes : 1);
   auto aligned = [](const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; };
   t.wide_y = aligned(p.y) && p.y_row % 8 == 0 && (!p.resid || (aligned(p.resid) && p.resid_row % 8 == 0));
-  t.wide_bias = aligned(p.bias);
   // (one row, one output: no stride of its own)
   const uint64_t k8 = ((uint64_t)p.k + 7) / 8 * 8;
   CUtensorMap mx, mw;
