@@ -362,43 +362,57 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_f32_kernel(const Params<EPI>
       *reinterpret_cast<float4*>(tile + tid * TILE_PITCH + c) = make_float4(acc[c / 2].x, acc[c / 2].y, acc[c / 2 + 1].x, acc[c / 2 + 1].y);
   }
   if constexpr (LINEAR) {
-    // ---- bias, activation, residual: a warp a row, two columns a lane
+    // ---- bias, activation, residual: a warp a row, two columns a lane; the residual of RB rows comes together, the first before the
+    // sums are there
+    constexpr int NW = kThreads / 32, RB = 5;
     const float* bias = p.bias;
     const int n0 = 2 * pair0, c[2] = {n0 + lane, n0 + 32 + lane};
-    float bv[2];
+    const int share = p.tile_rows / splits, r_first = splits > 1 ? (int)blockIdx.z * share : 0, r_end = min(r_first + share, rows_of_tile);
+    float bv[2], add[RB][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) bv[i] = bias && c[i] < p.n ? bias[c[i]] : 0.f;
-    const int share = p.tile_rows / splits, r0 = splits > 1 ? (int)blockIdx.z * share : 0;
+    auto read_resid = [&](int r0) {
+#pragma unroll
+      for (int k = 0; k < RB; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          add[k][i] = p.resid && r0 + NW * k < r_end && c[i] < p.n
+                          ? reinterpret_cast<const float*>(p.resid)[(long long)(m0 + r0 + NW * k) * p.resid_row + c[i]] : 0.f;
+    };
+    read_resid(r_first + warp);
     if (splits > 1) cluster_sync_all();
     else __syncthreads();
-    for (int r = r0 + warp; r < r0 + share && r < rows_of_tile; r += kThreads / 32) {
-      const long long row = m0 + r;
-      float v[2] = {tile[r * TILE_PITCH + lane], tile[r * TILE_PITCH + 32 + lane]};
-      if (splits > 1) {
-        const uint32_t at = smem_u32(tile + r * TILE_PITCH + lane);
-        v[0] = v[1] = 0.f;
-        for (int s = 0; s < splits; ++s) {
-          const uint32_t from = map_to_cta(at, (uint32_t)s);
-          v[0] += __uint_as_float(ld_cluster_u32(from));
-          v[1] += __uint_as_float(ld_cluster_u32(from + 128));
-        }
-      }
-      if (!finite(v[0]) || !finite(v[1])) {
-        const int last = p.n - 1;
-        const float2 ab = plain_dots(reinterpret_cast<const float*>(p.x) + row * p.x_row, w + (long long)min(c[0], last) * p.w_row,
-                                     w + (long long)min(c[1], last) * p.w_row, K);
-        if (!finite(v[0])) v[0] = ab.x;
-        if (!finite(v[1])) v[1] = ab.y;
-      }
-      v[0] += bv[0];
-      v[1] += bv[1];
-      activate<false>(v, p.act);
+    for (int r0 = r_first + warp; r0 < r_end; r0 += NW * RB) {
+      if (r0 != r_first + warp) read_resid(r0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (c[i] < p.n) {
-          if (p.resid) v[i] += reinterpret_cast<const float*>(p.resid)[row * p.resid_row + c[i]];
-          reinterpret_cast<float*>(p.y)[row * p.y_row + c[i]] = v[i];
+      for (int k = 0; k < RB; ++k) {
+        const int r = r0 + NW * k;
+        if (r >= r_end) break;
+        const long long row = m0 + r;
+        float v[2] = {tile[r * TILE_PITCH + lane], tile[r * TILE_PITCH + 32 + lane]};
+        if (splits > 1) {
+          const uint32_t at = smem_u32(tile + r * TILE_PITCH + lane);
+          v[0] = v[1] = 0.f;
+          for (int s = 0; s < splits; ++s) {
+            const uint32_t from = map_to_cta(at, (uint32_t)s);
+            v[0] += __uint_as_float(ld_cluster_u32(from));
+            v[1] += __uint_as_float(ld_cluster_u32(from + 128));
+          }
         }
+        if (!finite(v[0]) || !finite(v[1])) {
+          const int last = p.n - 1;
+          const float2 ab = plain_dots(reinterpret_cast<const float*>(p.x) + row * p.x_row, w + (long long)min(c[0], last) * p.w_row,
+                                       w + (long long)min(c[1], last) * p.w_row, K);
+          if (!finite(v[0])) v[0] = ab.x;
+          if (!finite(v[1])) v[1] = ab.y;
+        }
+        v[0] += bv[0];
+        v[1] += bv[1];
+        activate<false>(v, p.act);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (c[i] < p.n) reinterpret_cast<float*>(p.y)[row * p.y_row + c[i]] = p.resid ? v[i] + add[k][i] : v[i];
+      }
     }
     __syncwarp();
     if (splits > 1) cluster_sync_all();          // nobody leaves while its sums are read
