@@ -108,9 +108,10 @@ dare_status_t dare_linear(const dare_linear_config_t* cfg, const void* x, const 
  * k_begin[b + 1] - k_begin[b].  Query head h reads key/value head h / (n_heads / n_kv_heads).
  *     out_i = sum_j softmax_j(scale q_i . k_j) v_j    over j < n_b and, if causal, j <= i + n_b - (query rows of b)
  * (the last query sees every key).  A row that sees no key gets zeros, and -inf as its lse = log sum_j exp(scale q_i . k_j).
- * Rows of q, out and lse outside every sequence are not touched; k and v are never read into results outside their sequence, and
- * a key that causality hides from every query of a tile never either; the v rows of a sequence that are hidden from some
- * queries only must be finite.  One query a sequence is a decoding step; a sequence may be empty. */
+ * Rows of q, out and lse outside every sequence are not touched; k and v are never read into results outside their sequence.
+ * The rows (query, head of the group) of a sequence are worked on in tiles of at most 256, in that order from its first: a key and value that
+ * causality hides from all of a tile's queries never come into its results; a v row that it hides from some of them only must be
+ * finite (its weight there is 0).  One query a sequence is a decoding step; a sequence may be empty. */
 typedef struct {
   uint32_t struct_size; /* sizeof(dare_attention_config_t) */
   int32_t dtype;        /* dare_dtype_t of q, k, v and out; softmax in float32 */

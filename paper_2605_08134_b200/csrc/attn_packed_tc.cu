@@ -52,7 +52,8 @@ __device__ __forceinline__ bool segment_at(WorkLine& line, unsigned u, unsigned 
   const int shift = p.unit_shift - 6;                                        // (blocks of 64 keys)
   *end = part.end;
   g->blk0 = (int)(part.k0 << shift);
-  g->n_blk = max(0, min(blocks_seen<BK>(p, *g, g->rows - 1), (int)(part.k1 << shift)) - g->blk0);
+  g->seen = row_sees(p, *g, g->rows - 1);
+  g->n_blk = max(0, min((g->seen + BK - 1) / BK, (int)(part.k1 << shift)) - g->blk0);
   g->slot = part.slot;
   g->none = part.k1 == 0;
   return true;
@@ -213,17 +214,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const int slot = ring0 + (int)(sc % RING);
           mbar_poll(&p_full[2 * st + sb], (sc >> 1) & 1, p.status);          // P(j) has replaced S(j)
           mbar_wait(&v_full[slot], (sc / RING) & 1, p.status);
-          // rows behind the sequence's last key are whatever lies there, and 0 * inf would be NaN: they become zeros
-          const int keys = g.pl.s.n - (g.blk0 + 2 * j + st) * BK;
-          if (keys < BK) {
-            uint8_t* v = smem + S::V_OFF + slot * S::KV_BYTES;
-            for (int i = lane; i < (BK - keys) * UPR; i += 32) {
-              const int r = keys + i / UPR, unit = i % UPR;
-              *reinterpret_cast<uint4*>(v + (unit >> 3) * (BK * 128) + r * 128 + ((unit & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
+          const int keys = g.seen - (g.blk0 + 2 * j + st) * BK;              // (at least one: the block is one that is seen)
+          if (keys < BK) zero_values<HD, BK>(smem + S::V_OFF + slot * S::KV_BYTES, keys, lane);
           tc_fence_after();
           if (elect_one()) {
             const uint64_t v_desc = v_desc0 + (uint64_t)(slot * (S::KV_BYTES >> 4));

@@ -93,14 +93,26 @@ struct Segment {
   Place pl;
   TileRows at;                   // where the CTA's rows begin
   int rows;                      // its rows
+  int seen;                      // keys that the last of them sees: none of its rows sees more
   int blk0, n_blk;               // blocks of keys [blk0, blk0 + n_blk)
   int slot;                      // < 0: the rows' keys are all here; else the slot of the partial result
   bool none;                     // the share ends before the pair's keys begin
 };
-// blocks of BLK keys that row `last_row` of the segment sees
-template <int BLK>
-__device__ __forceinline__ int blocks_seen(const PackedParams& p, const Segment& g, int last_row) {
-  return (keys_seen(p, g.pl.s, row_at(p, g.at, 0, last_row).query) + BLK - 1) / BLK;
+// keys that row `row` of the segment sees
+__device__ __forceinline__ int row_sees(const PackedParams& p, const Segment& g, int row) {
+  return keys_seen(p, g.pl.s, row_at(p, g.at, 0, row).query);
+}
+// Values of a block of BLK keys (HD / 64 chunks of 64 columns) from row `keys` on become zeros, by the warp that issues their product: what
+// lies there is hidden from all rows or another sequence's, may be anything, and 0 * inf would be NaN.
+template <int HD, int BLK>
+__device__ __forceinline__ void zero_values(uint8_t* v, int keys, int lane) {
+  constexpr int UPR = HD / 8;
+  for (int i = lane; i < (BLK - keys) * UPR; i += 32) {
+    const int r = keys + i / UPR, unit = i % UPR;
+    *reinterpret_cast<uint4*>(v + (unit >> 3) * (BLK * 128) + r * 128 + ((unit & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
 }
 
 }  // namespace packed_tc

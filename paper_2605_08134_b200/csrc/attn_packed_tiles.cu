@@ -35,7 +35,8 @@ __device__ __forceinline__ bool tile_segment(Line<2 * BQ, false>& line, unsigned
   g->at = tile_rows(p, row0);
   g->rows = min(2 * BQ, g->pl.s.nq * p.group - row0);
   g->blk0 = 0;
-  g->n_blk = blocks_seen<TK>(p, *g, g->rows - 1);
+  g->seen = row_sees(p, *g, g->rows - 1);
+  g->n_blk = (g->seen + TK - 1) / TK;
   g->slot = -1;
   g->none = false;
   return true;
@@ -131,7 +132,7 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 
     const int st = warp < 4 ? (warp & 1) : ((warp - 4) >> 2);            // stream
     const int rows = stream_rows(g, st);
-    const int n_st = rows > 0 ? min(g.n_blk, blocks_seen<TK>(p, g, st * BQ + rows - 1)) : 0;
+    const int n_st = rows > 0 ? min(g.n_blk, (row_sees(p, g, st * BQ + rows - 1) + TK - 1) / TK) : 0;
     const uint32_t tmem_s = tmem_base + st * TK, tmem_o = tmem_base + 2 * TK + st * HD;
     if (warp < 4) {
       set_registers_down<40>();
@@ -167,17 +168,8 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         for (int j = 0; j < n_st; ++j) {
           const int slot = j & 1;
           mbar_wait(&v_full[slot], (j >> 1) & 1, p.status);
-          // rows behind the sequence's last key are whatever lies there, and 0 * inf would be NaN: they become zeros
-          const int keys = g.pl.s.n - j * TK;
-          if (keys < TK) {
-            uint8_t* v = smem + S::V_OFF + slot * S::KV_BYTES;
-            for (int i = lane; i < (TK - keys) * UPR; i += 32) {
-              const int r = keys + i / UPR, unit = i % UPR;
-              *reinterpret_cast<uint4*>(v + (unit >> 3) * (TK * 128) + r * 128 + ((unit & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
+          const int keys = g.seen - j * TK;          // (of the tile: the streams share the block, both may write the same zeros)
+          if (keys < TK) zero_values<HD, TK>(smem + S::V_OFF + slot * S::KV_BYTES, keys, lane);
           const uint64_t v_desc = v_desc0 + (uint64_t)(slot * (S::KV_BYTES >> 4));
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                                   // 64 keys of P each
