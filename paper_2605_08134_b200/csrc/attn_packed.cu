@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(con
   __shared__ int more_sh;
   // (the lengths are inputs: complete before the kernel in front let this one start)
   if (threadIdx.x < 32) {
-    Line<ROWS, true> line(p);
+    Line<ROWS, true, true> line(p);
     const unsigned per = share_units(p, line.total()), cut = (blockIdx.x + 1) * per;
     Place pl;
     const bool found = line.find(cut, &pl) && pl.first < cut && pl.first >= cut - per;

@@ -45,13 +45,16 @@ struct PackedParams {
 struct SeqGeom {
   int q0, nq, k0, n;             // query rows, key rows
 };
-// A sequence whose slices are not inside the arrays is flagged and has no rows.
+// A sequence whose slices are not inside the arrays is flagged and has no rows.  PAST_L1: for the merge kernel, which looks lengths up
+// before it waits (behind the wait of the kernel in front: what was written before that is in the L2).
+template <bool PAST_L1>
 __device__ __forceinline__ SeqGeom seq_geom(const PackedParams& p, int b) {
+  auto at = [](const int* x) { return PAST_L1 ? __ldcg(x) : *x; };
   SeqGeom s;
-  s.q0 = __ldg(p.q_begin + b);
-  const long long q1 = __ldg(p.q_begin + b + 1);
-  s.k0 = __ldg(p.k_begin + b);
-  const long long n = p.k_len ? (long long)__ldg(p.k_len + b) : (long long)__ldg(p.k_begin + b + 1) - s.k0;
+  s.q0 = at(p.q_begin + b);
+  const long long q1 = at(p.q_begin + b + 1);
+  s.k0 = at(p.k_begin + b);
+  const long long n = p.k_len ? (long long)at(p.k_len + b) : (long long)at(p.k_begin + b + 1) - s.k0;
   if (s.q0 < 0 || q1 < s.q0 || q1 > p.q_rows || s.k0 < 0 || n < 0 || s.k0 + n > p.k_rows) {
     flag_device_check(p.status);
     s.q0 = s.nq = s.k0 = s.n = 0;
@@ -98,7 +101,7 @@ struct UnitCount {
 // sequence l of the 32 looked at last, so that with at most 32 sequences the lengths are read once.  Everything in 32 bits (the host
 // sees to it that the line is no longer): this is on the way to a CTA's first key, and fetching the instructions of 64-bit
 // divisions through the L2 behind other CTAs' keys took some of them 4 us.
-template <int BQ, bool UNITS>
+template <int BQ, bool UNITS, bool PAST_L1 = false>
 struct Line {
   const PackedParams& p;
   SeqGeom s;
@@ -114,7 +117,7 @@ struct Line {
     const int lane = threadIdx.x & 31, b = first + lane;
     b0 = first;
     s = SeqGeom{0, 0, 0, 0};
-    if (b < p.batch) s = seq_geom(p, b);
+    if (b < p.batch) s = seq_geom<PAST_L1>(p, b);
     tiles = (int)(((unsigned)s.nq * (unsigned)p.group + BQ - 1) / BQ);
     head = (unsigned)tiles;
     if (UNITS) {

@@ -117,16 +117,19 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
 #pragma unroll
         for (int j = 0; j < kOut; ++j) {
           raw[u][j] = make_uint4(0u, 0u, 0u, 0u);
-          if (c + u * stride < whole) raw[u][j] = __ldg(reinterpret_cast<const uint4*>(w[j]) + c + u * stride);
+          if (c + u * stride < whole) raw[u][j] = reinterpret_cast<const uint4*>(w[j])[c + u * stride];
         }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int at = c + u * stride;
         if (at >= whole) break;
+        uint4 own[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) own[i] = reinterpret_cast<const uint4*>(x[i])[at];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           float2 b[VE / 2];
-          widen<T, VE>(__ldg(reinterpret_cast<const uint4*>(x[i]) + at), b);
+          widen<T, VE>(own[i], b);
 #pragma unroll
           for (int j = 0; j < kOut; ++j) {
             float2 a[VE / 2];

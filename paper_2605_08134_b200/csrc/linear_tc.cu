@@ -173,7 +173,7 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         for (int i = 0; i < kBiasCols; i += 32) {
           const int e = i + lane, run = t.wide_y ? 31 : 15;          // the warps of a quarter take runs of 32 (16) columns in turn
           const int c = 2 * (e & ~run) + sub * (run + 1) + (e & run);
-          if (c < cols) bias_sh[e] = __ldg(p.bias + n0 + c);
+          if (c < cols) bias_sh[e] = p.bias[n0 + c];
         }
         __syncwarp();
       }
@@ -346,7 +346,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_const
     if (e >= last || n >= p.n) return;
     if (p.bias) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) bias[i] = __ldg(p.bias + min(n + i, p.n - 1));
+      for (int i = 0; i < 8; ++i) bias[i] = p.bias[min(n + i, p.n - 1)];
     }
     if (p.resid && t.wide_y && n + 8 <= p.n)
       rs = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(p.resid) + (long long)(m0 + r) * p.resid_row + n);

@@ -1,4 +1,9 @@
 // What the stand-alone operators of dare_ops.h share between their translation units.
+//
+// Their kernels are launched while the kernel in front of them may still run (launch_pdl), and any operand may be what that one writes.
+// So nothing of an operand is read before pdl_wait() (the lengths in attention's merge: before its own, behind the one of the kernel in
+// front), and none of it by a read-only load: those are for data that does not change while the kernel lives, and may be moved in
+// front of the wait.
 #pragma once
 
 #include "dare_internal.h"

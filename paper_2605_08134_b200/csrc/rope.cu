@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p) {
     const int tl = w / per_token, rest = w - tl * per_token, chunk = rest / p.units, u = rest - chunk * p.units;
     const long long t = t0 + tl;
     if (t >= p.tokens) return;
-    const long long pos = p.positions ? (long long)__ldg(p.positions + t) : p.pos_begin + t;
+    const long long pos = p.positions ? (long long)p.positions[t] : p.pos_begin + t;
     const int h0 = chunk * kHeads, n = min(kHeads, p.heads - h0);
     const T* x = reinterpret_cast<const T*>(p.x) + t * p.x_token + h0 * p.x_head;
     T* y = reinterpret_cast<T*>(p.y) + t * p.y_token + h0 * p.y_head;
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_kernel(const RopeParams p) {
     float2 cs[PAIRS];
 #pragma unroll
     for (int k = 0; k < PAIRS; ++k) {
-      cs[k] = __ldg(tab + k);
+      cs[k] = tab[k];
       cs[k].y *= sign;
     }
 #pragma unroll
