@@ -130,7 +130,8 @@ typedef struct {
 size_t dare_attention_workspace_bytes(const dare_attention_config_t* cfg);
 
 /* q_begin int32 [batch + 1]; k_begin int32 [batch + 1], or [batch] with k_len int32 [batch]; lse float32 [q_rows, n_heads] or NULL.
- * A sequence whose slices are not inside q_rows / k_rows is skipped (DARE_ERR_DEVICE_CHECK); query slices must not overlap.
+ * A sequence whose slices are not inside q_rows / k_rows is skipped (DARE_ERR_DEVICE_CHECK); query slices must not overlap (where
+ * q_begin runs back and forth, rows may be left out, all of them where the work passes 2^31 units).
  * bf16 with head_dim 64 or 128, q, k, v, out 16-byte aligned and strides multiples of 8 runs on the tensor cores, everything else on
  * the CUDA cores. */
 dare_status_t dare_attention(const dare_attention_config_t* cfg, const void* q, const void* k, const void* v,

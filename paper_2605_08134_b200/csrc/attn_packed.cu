@@ -295,9 +295,9 @@ __global__ void __launch_bounds__(kCombineThreads, 18) packed_combine_kernel(con
   // (the lengths are inputs: complete before the kernel in front let this one start)
   if (threadIdx.x < 32) {
     Line<ROWS, true, true> line(p);
-    const unsigned per = share_units(p, line.total()), cut = (blockIdx.x + 1) * per;
+    const unsigned total = line.total(), per = share_units(p, total), cut = (blockIdx.x + 1) * per;
     Place pl;
-    const bool found = line.find(cut, &pl) && pl.first < cut && pl.first >= cut - per;
+    const bool found = cut < total && line.find(cut, &pl) && pl.first < cut && pl.first >= cut - per;
     if (threadIdx.x == 0) { pl_sh = pl; per_sh = per; more_sh = found ? 1 : 0; }
   }
   __syncthreads();

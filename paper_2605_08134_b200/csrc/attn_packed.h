@@ -108,6 +108,9 @@ struct Line {
   int tiles, b0;                 // of this lane's sequence; first sequence of the 32
   UnitCount count;
   unsigned base, head, inc;      // units before the 32; of a head of this lane's sequence; up to and with its last head
+  // Query slices that do not overlap stay below 2^31 units.  Those that run back and forth may not: sums stop there.
+  static constexpr unsigned kFull = 1u << 31;
+  static __device__ __forceinline__ unsigned sum(unsigned a, unsigned b) { return a + min(b, kFull - a); }    // (a, b <= kFull)
 
   __device__ __forceinline__ explicit Line(const PackedParams& p_) : p(p_) {
     load(0);
@@ -139,13 +142,13 @@ struct Line {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const unsigned v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
+      if (lane >= o) inc = sum(inc, v);
     }
   }
   // next 32 sequences; false: there are none
   __device__ __forceinline__ bool next() {
     if (b0 + 32 >= p.batch) return false;
-    base += __shfl_sync(0xffffffffu, inc, 31);
+    base = sum(base, __shfl_sync(0xffffffffu, inc, 31));
     load(b0 + 32);
     return true;
   }
@@ -153,10 +156,14 @@ struct Line {
     if (b0 != 0) load(0);
     base = 0;
   }
+  // 0 too for a line that is longer than its sums can tell, which is flagged: nothing of it is worked on.
   __device__ __forceinline__ unsigned total() {
     rewind();
     while (next()) {}
-    return base + __shfl_sync(0xffffffffu, inc, 31);
+    const unsigned all = sum(base, __shfl_sync(0xffffffffu, inc, 31));
+    if (all < kFull) return all;
+    flag_device_check(p.status);
+    return 0u;
   }
   // Pair that holds unit u; the same for all lanes.  false: u is behind the last one.
   __device__ __forceinline__ bool find(unsigned u, Place* out) {
@@ -172,9 +179,8 @@ struct Line {
     out->tiles = __shfl_sync(0xffffffffu, tiles, src);
     const unsigned per_head = __shfl_sync(0xffffffffu, head, src);
     const unsigned in_seq = u - base - __shfl_sync(0xffffffffu, inc - head * (unsigned)p.kv_heads, src);
-    // (head by head; the bound holds by itself unless slices that overlap make the line longer than 32 bits)
-    out->h = min((int)(in_seq / per_head), p.kv_heads - 1);
-    const unsigned in_head = min(in_seq - (unsigned)out->h * per_head, per_head - 1);
+    out->h = (int)(in_seq / per_head);
+    const unsigned in_head = in_seq - (unsigned)out->h * per_head;
     if (!UNITS) {
       out->tile = out->tiles - 1 - (int)in_head;                              // the longest first
       out->units = 1;

@@ -46,3 +46,16 @@ def test_values_hidden_from_a_whole_tile(dare, dtype, hd, heads, kv_heads, nq, n
         whole = (t + 1) * tile_rows // group                   # queries that are in no other tile
         assert torch.equal(got[:whole], want[:whole]) and torch.equal(lse[:whole], want_lse[:whole]), t
         assert not bool(got[queries:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,hd,batch", [(BF16, 128, 1750), (BF16, 64, 3000), (F32, 32, 700)])
+def test_slices_back_and_forth_past_all_sums(dare, dtype, hd, batch):
+    """Offsets that go to the end and back until the units of work pass 2^31: flagged, and nothing is computed."""
+    rows, heads = 100000, 8
+    q, k, v = (torch.zeros((rows, heads, hd), dtype=dtype, device="cuda") for _ in range(3))
+    status, out = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full_like(q, 7.0)
+    call = lambda b, o: dare.attention(q, k, v, ints([0, rows] * (b // 2)), ints([0] * (b - 1)), k_len=ints([rows] * (b - 1)), out=o,
+                                       status=status, return_lse=True)
+    call(batch, out)
+    assert status.item() == dare.ERR_DEVICE_CHECK
+    assert bool((out == 7.0).all())
