@@ -90,10 +90,13 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
   if (tc) {
     // 256 rows a CTA, or shares?  What each takes, in us, from k_rows / batch keys a sequence (a cache may hold fewer): a CTA of the first
     // takes 2 us a 128 keys (1.2 with rows for one stream only), the launch 6; the shares take 1.1 us a 128 keys and tile of 128 rows
-    // (0.75 with few rows) over all SMs, five such for a tile itself, and 13 with the merge.  Tiles / shares in us, heads of 128, 32
-    // query and 8 key heads: a prompt of 300 tokens 12.4 / 18.0, 4000 148 / 167, four of up to 1500 81 / 102; 4 and 1 heads: 4000
-    // tokens 62 / 44; two blocks of 256 tokens over 8192 keys 124 / 78, four of 512 151 / 173, one token over 4000 keys 42 / 17, four
-    // over 200 8.4 / 11.  Of 64 such shapes (heads of 64 too) the rule takes the slower form, by more than 5 %, in six, by 33 % at most.  Each CTA of the first looks its
+    // (0.75 with few rows) over all SMs, five such for a tile itself, and 13 with the merge.  Heads of 64 have two products a weight, which
+    // the shares hide better: 1 us (0.7), three for a tile, 11 with the merge, and only the keys that causality leaves count.
+    // Tiles / shares in us, heads of 128, 32 query and 8 key heads: a prompt of 300 tokens 12 / 17, 4000 137 / 180, four of up to 1500
+    // 66 / 96; 4 and 1 heads: 4000 tokens 56 / 38; two blocks of 256 tokens over 8192 keys 108 / 78, four of 512 225 / 284, one token over
+    // 4000 keys 49 / 16, four over 200 8.3 / 11.6.  Heads of 64: a prompt of 300 tokens 12.2 / 13.0, 4000 161 / 149, four of up to 1500
+    // 68 / 75; 8 and 8 heads: 4000 tokens 68 / 48, four of up to 700 18 / 16; 4 and 1 heads: four of up to 4000 69 / 52.  Of 108 such
+    // shapes the rule takes the slower form, by more than 5 %, in nine, by 34 % at most.  Each CTA of the first looks its
     // pair up among the sequences' lengths, the shares twice a launch: 256 prompts of up to 200 tokens, 8 and 8 heads, 163 / 161 us,
     // 1024 1048 / 607.
     const float keys = (float)(c->k_rows / c->batch) / 128.f + 1.f;
@@ -102,7 +105,9 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
     const float pairs = (float)((all / 128 > c->batch ? all / 128 : c->batch) * c->n_kv_heads);
     const float look_up = 0.012f * (float)c->batch;
     const float tiles_us = (6.f + look_up + keys * (rows_each > 128 ? 2.f : 1.2f)) * fmaxf(1.f, ctas / (float)kSms);
-    const float shares_us = 13.f + pairs * (keys + 5.f) * (rows_each > 64 ? 1.1f : 0.75f) / (float)kSms;
+    const float seen = c->causal ? 1.f - 0.5f * fminf(1.f, (float)c->q_rows / (float)c->k_rows) : 1.f;
+    const float shares_us = c->head_dim == 64 ? 11.f + pairs * (keys * seen + 3.f) * (rows_each > 64 ? 1.f : 0.7f) / (float)kSms
+                                              : 13.f + pairs * (keys + 5.f) * (rows_each > 64 ? 1.1f : 0.75f) / (float)kSms;
     const bool tiles = (rows_each > 128 && ctas >= (float)kSms && c->batch <= 256) || tiles_us <= shares_us;
     e = launch_packed_tc(p, c->head_dim, tiles, st);
     if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);

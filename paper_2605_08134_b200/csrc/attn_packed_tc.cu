@@ -5,9 +5,10 @@
 //             tensor memory
 //   softmax   four warps a stream, thread <-> row: scores from tensor memory, maximum, 2^x, P as bf16 back over the scores; O is rescaled
 //             in place only when a row's maximum grew by more than 2^8
-// P is one bf16 part: its rounding (2^-8 of a weight at most) leaves the output 1.3 to 1.4 times as far from exact as storing it as
-// bf16 does.  A second part for what the rounding left would bring that to 1.0, and took 10 % (a block of 160 over 2500 keys) to 30 %
-// (prompts) more time with heads of 64, half as much tensor work again with heads of 128.
+// P is one bf16 part with heads of 128: its rounding (2^-8 of a weight at most) leaves the output 1.3 to 1.4 times as far from exact as
+// storing it as bf16 does; a second part would be half as much tensor work again.  With heads of 64 it is two parts, 16 bits, as in the
+// layer's own attention: the output is as near to exact as its storage is (1.66e-3 relative; one part: 2.3e-3).  The second part
+// takes 10 % (a block of 160 over 2500 keys) to 30 % (prompts) of a call's time.
 // Shares: a CTA has 128 rows and its streams take its blocks of 64 keys in turn, so that few rows (a decoding step has n_heads /
 // n_kv_heads of them) still keep 192 KB of keys and values on their way; the streams' results are merged as two parts of a key
 // split.  Two score buffers a stream: the next block's scores are there when the softmax is through with one.  The producers know a
@@ -222,6 +223,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
             for (int ks = 0; ks < BK / 16; ++ks) {
               umma_ts(tmem_o, tmem_s + sb * BK + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, (j | ks) != 0 ? 1u : 0u);
+              if (kSplitP<HD>) umma_ts(tmem_o, tmem_s + sb * BK + 32 + ks * 8, v_desc + ((ks * (16 * 128)) >> 4), idesc_pv, 1u);
             }
             umma_commit(&o_full[2 * st + sb]);
             umma_commit(&v_empty[slot]);
@@ -289,17 +291,17 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const float mc = m == -INFINITY ? 0.f : m * c;             // (nothing seen yet: 2^-inf = 0, not 2^NaN)
           const float2 c2 = make_float2(c, c), nmc2 = make_float2(-mc, -mc);
           float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          float pk[BK / 2];
+          float pk[BK / 2], pl[kSplitP<HD> ? BK / 2 : 1];
 #pragma unroll
           for (int i = 0; i < BK; i += 2) {
             float2 e = __ffma2_rn(make_float2(v[i], v[i + 1]), c2, nmc2);
             e.x = fast_exp2(e.x);
             e.y = fast_exp2(e.y);
             sum2[(i >> 1) & 1] = __fadd2_rn(sum2[(i >> 1) & 1], e);
-            __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
-            pk[i >> 1] = __uint_as_float(*reinterpret_cast<uint32_t*>(&h2));
+            pack_weights<kSplitP<HD>>(e, pk[i >> 1], pl[kSplitP<HD> ? i >> 1 : 0]);
           }
           tmem_st_32x32_nowait(sbuf, pk);
+          if constexpr (kSplitP<HD>) tmem_st_32x32_nowait(sbuf + 32, pl);
           tmem_st_wait();
           l += (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
           tc_fence_before();

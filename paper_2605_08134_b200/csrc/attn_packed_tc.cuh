@@ -12,36 +12,27 @@ using namespace ptx;
 constexpr int BQ = kTcRows, kThreads = 384, kSoftmaxThreads = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr float kRescaleStep = 8.f;        // log2 of the growth of a row's maximum that has O rescaled
+// Heads of 64: P as two bf16 parts, the rounded weight and what the rounding left (16 bits together), each multiplied with V: together they
+// take the columns that the scores had.  As in the layer's attention: see attn_packed_tc.cu.
+template <int HD>
+constexpr bool kSplitP = HD == 64;
+// Two weights as bf16, and of two parts what that leaves of them.
+template <bool SPLIT>
+__device__ __forceinline__ void pack_weights(float2 e, float& high, float& low) {
+  const __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
+  high = __uint_as_float(*reinterpret_cast<const uint32_t*>(&h2));
+  if constexpr (SPLIT) {
+    const float2 rest = __fadd2_rn(e, make_float2(-__low2float(h2), -__high2float(h2)));
+    const __nv_bfloat162 l2 = __floats2bfloat162_rn(rest.x, rest.y);
+    low = __uint_as_float(*reinterpret_cast<const uint32_t*>(&l2));
+  }
+}
 constexpr int one_cta_per_sm(int bytes) { return bytes > 117 * 1024 ? bytes : 117 * 1024; }   // (a CTA takes all tensor memory)
 
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-// The same of two numbers in multiply-adds: 2^x = 2^n p(x - n), n = x rounded, p the polynomial of degree 5 with the least relative error
-// on [-1/2, 1/2] (a weighted least-squares fit, weights raised where the error is large, until it is level): 2^-23.6.  Below
-// -126.5 exactly 0; NaN stays NaN.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
-__device__ __forceinline__ float2 poly_exp2(float2 x) {
-  constexpr float kRound = 12582912.f;                                // 1.5 2^23: its unit is 1
-  auto both = [](float v) { return make_float2(v, v); };
-  x.x = max_nan(x.x, -127.f);
-  x.y = max_nan(x.y, -127.f);
-  const float2 r = __fadd2_rn(x, both(kRound));                       // n in the low bits
-  const float2 f = __ffma2_rn(__fadd2_rn(r, both(-kRound)), both(-1.f), x);
-  float2 p = __ffma2_rn(f, both(1.327647245489061e-3f), both(9.675541892647743e-3f));
-  p = __ffma2_rn(p, f, both(5.550713092088699e-2f));
-  p = __ffma2_rn(p, f, both(2.4022120237350464e-1f));
-  p = __ffma2_rn(p, f, both(6.931469440460205e-1f));
-  p = __ffma2_rn(p, f, both(1.0000001192092896f));
-  const float2 scale = make_float2(__int_as_float((__float_as_int(r.x) << 23) + 0x3f800000),
-                                   __int_as_float((__float_as_int(r.y) << 23) + 0x3f800000));
-  return __fmul2_rn(p, scale);
 }
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
   float d;

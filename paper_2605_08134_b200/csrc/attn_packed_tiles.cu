@@ -49,10 +49,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PackedParams p) {
   using S = TileSmem<HD>;
   constexpr int UPR = HD / 8;
-  // Heads of 64 are bound by the exponentials: every fourth pair of them is worked out in multiply-adds.  Four causal prompts of up to
-  // 4000 tokens, 32 heads, us: none 296, every sixth 284, fourth 280, third 286, second 312; 512 queries over 8192 keys 137 / 128.
-  // Heads of 128 have twice the products to each: none 388, every eighth 389, fourth 405.
-  constexpr int POLY = HD == 64 ? 4 : 0;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);    // [2]
@@ -180,6 +176,7 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
               for (int ks = 0; ks < 4; ++ks) {
                 const uint64_t v16 = v_desc + (((h * 4 + ks) * (16 * 128)) >> 4);
                 umma_ts(tmem_o, tmem_s + h * 32 + ks * 8, v16, idesc_pv, (j | h | ks) != 0 ? 1u : 0u);
+                if (kSplitP<HD>) umma_ts(tmem_o, tmem_s + 64 + h * 32 + ks * 8, v16, idesc_pv, 1u);
               }
               if (h == 1) {
                 umma_commit(&v_empty[slot]);
@@ -255,7 +252,7 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         // The exponentials are taken against the maximum of the blocks before, so that they need not wait for this one's; only if it
         // has grown by more than 2^8 (any smaller growth changes nothing in exact arithmetic) are the first half's taken again.
         float2 sum2[2];
-        float pk[16];
+        float pk[16], pl[kSplitP<HD> ? 16 : 1];
         auto exponentials = [&](auto part) {                               // of 32 keys
           constexpr int k0 = decltype(part)::value * 32;
           const float mc = m == -INFINITY ? 0.f : m * c;                   // (nothing seen yet: 2^-inf = 0, not 2^NaN)
@@ -263,18 +260,16 @@ packed_tiles_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             float2 e = __ffma2_rn(make_float2(v[k0 + i], v[k0 + i + 1]), c2, nmc2);
-            if (POLY > 0 && (i >> 1) % POLY == POLY - 1) {
-              e = poly_exp2(e);
-            } else {
-              e.x = fast_exp2(e.x);
-              e.y = fast_exp2(e.y);
-            }
+            e.x = fast_exp2(e.x);
+            e.y = fast_exp2(e.y);
             sum2[(i >> 1) & 1] = __fadd2_rn(sum2[(i >> 1) & 1], e);
-            __nv_bfloat162 h2 = __floats2bfloat162_rn(e.x, e.y);
-            pk[i >> 1] = __uint_as_float(*reinterpret_cast<uint32_t*>(&h2));
+            pack_weights<kSplitP<HD>>(e, pk[i >> 1], pl[kSplitP<HD> ? i >> 1 : 0]);
           }
         };
-        auto store_p = [&](int part) { tmem_st_32x16_nowait(sbuf + part * 16, pk); };
+        auto store_p = [&](int part) {
+          tmem_st_32x16_nowait(sbuf + part * 16, pk);
+          if constexpr (kSplitP<HD>) tmem_st_32x16_nowait(sbuf + 64 + part * 16, pl);
+        };
         auto hand_over = [&](int h) {
           tmem_st_wait();
           tc_fence_before();

@@ -27,7 +27,7 @@ def make(nq, n, heads, kv_heads, hd, dtype, seed):
 
 # Rows of a tile: 256 (many rows), 128 (few rows over many keys), 32 or 8 (CUDA cores), counted over (query, head of the group).
 @pytest.mark.parametrize("dtype,hd,heads,kv_heads,nq,n,tile_rows", [
-    (BF16, 128, 8, 2, 300, 300, 256), (BF16, 64, 8, 2, 300, 300, 256), (BF16, 64, 4, 4, 700, 741, 256), (BF16, 128, 3, 1, 500, 530, 256),
+    (BF16, 128, 8, 2, 300, 300, 256), (BF16, 64, 8, 2, 300, 300, 256), (BF16, 64, 4, 4, 700, 741, 256), (BF16, 64, 64, 8, 700, 741, 256), (BF16, 128, 3, 1, 500, 530, 256),
     (BF16, 128, 8, 2, 64, 4010, 128), (BF16, 64, 8, 2, 64, 4010, 128), (BF16, 128, 14, 2, 50, 3001, 128), (BF16, 64, 1, 1, 290, 6000, 128),
     (F32, 64, 4, 2, 100, 133, 32), (F32, 128, 2, 2, 70, 900, 32), (BF16, 256, 4, 1, 40, 77, 32), (BF16, 32, 2, 2, 70, 600, 32)])
 def test_values_hidden_from_a_whole_tile(dare, dtype, hd, heads, kv_heads, nq, n, tile_rows):
