@@ -97,6 +97,7 @@ typedef struct {
 
 /* x [rows, in_features], w [out_features, in_features] (the layer's convention, y = W x), bias float32 [out_features] or NULL, resid
  * [rows, out_features] or NULL; resid may be y with the same stride.
+ * Activations are right to a few units of their value, small ones too; GELU in bf16 to 2^-24 of its argument.
  * bf16 with x, w 16-byte aligned and their strides multiples of 8 runs on the tensor cores, float32 with x, w 16-byte aligned,
  * strides and in_features multiples of 4 too where that is faster (operands split into three bf16 parts, fp32 accuracy); everything
  * else on the CUDA cores. */

@@ -19,8 +19,12 @@ struct LinearParams {
 };
 
 #ifdef __CUDACC__
-// v[i] = act(v[i]); one switch for all of them.  FAST: exponential and quotient on the special-function unit, right to 2^-20, far below
-// the rounding of a bf16 result (with the exact ones 37 rows of 12288 outputs took 4 us longer).
+// v[i] = act(v[i]); one switch for all of them.  FAST (bf16 results): exponential and quotient on the special-function unit.  __expf(x) is off
+// by 2 + 1.173 |x| units at most, so SiLU and tanh GELU are right to 2^-15 of their value wherever that is no underflow, far below a
+// bf16 result's rounding (with the exact ones 37 rows of 12288 outputs took 4 us longer).  1 + erf cancels for negative v: 2^-24 |v| then,
+// which below v = -4.5 is more than a bf16 result's rounding (results under 2e-5); erfc would be right there, and take up to
+// 35 % of a product of few k-elements (8192 x 512 x 512 13.1 / 17.7 us).  float32 has erfc, 2 % of 601 x 1024 x 1000, and no tanh,
+// which cancels the same way.
 template <bool FAST, int N>
 __device__ __forceinline__ void activate(float (&v)[N], int act) {
   switch (act) {
@@ -34,13 +38,13 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
       break;
     case DARE_ACT_GELU:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (FAST ? 1.f + erff(v[i] * 0.70710678118654752f) : erfcf(v[i] * -0.70710678118654752f));
       break;
     case DARE_ACT_GELU_TANH:
 #pragma unroll
       for (int i = 0; i < N; ++i) {                        // 0.5 (1 + tanh(u)) = 1 / (1 + e^-2u)
         const float u = 0.79788456080286536f * (v[i] + 0.044715f * v[i] * v[i] * v[i]);
-        v[i] = FAST ? __fdividef(v[i], 1.f + __expf(-2.f * u)) : 0.5f * v[i] * (1.f + tanhf(u));
+        v[i] = FAST ? __fdividef(v[i], 1.f + __expf(-2.f * u)) : v[i] / (1.f + expf(-2.f * u));
       }
       break;
     default: break;

@@ -66,3 +66,31 @@ def test_not_numbers_in_the_last_part(dare, m, k, n):
     assert torch.equal(got[:m - 1, :n - 1], plain[:m - 1, :n - 1])
     assert bool(got[:, n - 1].isnan().all()) and bool(got[m - 1, :n - 1].isinf().all())
     assert torch.equal(got[m - 1, :n - 1].sign(), w[:n - 1, k - 1].sign())
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 4, 3001), (4, 64, 1000), (30, 64, 500), (1000, 512, 640)])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_activations_keep_small_results(dare, act, m, k, n):
+    """Where an activation is nearly zero it is still right in relation to its value: arguments one after the other, products with one."""
+    v = torch.linspace(-9, 9, m * n, device="cuda").view(m, n)
+    if m > 4:
+        v = v[:, :1].expand(m, n)                            # (an argument a row)
+    x, w = torch.zeros((m, k), device="cuda"), torch.zeros((n, k), device="cuda")
+    # (the products are exact: one factor is 1, or for few rows a power of two)
+    if m > 4:
+        x[:, 0], w[:, 0] = v[:, 0], 1
+        arg = v.double()
+    else:
+        x[:, 0], w[:, 0] = 2.0 ** torch.arange(0, -m, -1, device="cuda"), v[0]
+        arg = x[:, :1].double() * w[:, 0].double()
+    got = dare.linear(x, w, act=dare.ACT[act]).double()
+    if act == "silu":
+        want, slope = arg / (1 + (-arg).exp()), arg.abs()
+    elif act == "gelu":
+        want, slope = 0.5 * arg * torch.special.erfc(-arg / 2 ** 0.5), arg.square()
+    else:
+        u = (2 / torch.pi) ** 0.5 * (arg + 0.044715 * arg ** 3)
+        want, slope = arg / (1 + (-2 * u).exp()), 8 * u.abs()
+    # A function of a rounded argument z (half a unit, for tanh's polynomial in z four units) is off by z times its logarithm's slope of
+    # them; the functions themselves and the operations around them by at most eight units of 2^-23.
+    assert bool(((got - want).abs() <= (8 + slope) * 2.0 ** -23 * want.abs()).all()), ((got - want).abs() / want.abs().clamp(min=1e-300)).max().item()
