@@ -13,9 +13,10 @@ namespace {
 // At most four rows: a stream of W.  k_warps warps of a CTA take kOut outputs together; their lanes share the k-elements, VE (16 bytes of
 // a row that allows it) a lane and step, and add their sums up at the end, halving the set of sums a lane holds at each step of the
 // exchange.  Sums of even and odd k-elements run side by side in packed multiply-adds.  k_warps is as large as fits two
-// CTAs an SM; float32 takes four at least, where that leaves each its own batch of loads.  bf16, one row, us with 1 / 2 / 4 / 8 (the pick
-// in brackets): 4096 x 6144 [11.9] / 13.2 / 12.6 / 13.9, 4096 x 4096 10.2 / [8.0] / 9.1 / 10.4, 1024 x 1000 2.8 / 2.3 / 2.1 / [2.1], three
-// rows of 8192 x 1024 28.4 / 15.7 / 9.2 / [6.5]; float32 4096 x 6144 19.9 / 19.4 / [18.2] / 17.6, 4096 x 12288 39.4 / 32.4 / [32.2] / 30.8.
+// CTAs an SM; float32 takes four at least, where that leaves each its own batch of loads.  W from the HBM, us with 1 / 2 / 4 / 8 (the pick
+// in brackets), bf16, one row: 4096 x 6144 [12.4] / 13.7 / 13.4 / 14.2, 4096 x 4096 10.7 / [8.4] / 9.6 / 10.5, 1024 x 1000 3.4 / 2.6 /
+// 2.4 / [2.4], three rows of 8192 x 1024 26.1 / 14.6 / 8.8 / [6.3]; float32 4096 x 6144 20.5 / 20.6 / [19.5] / 19.2, 4096 x 12288 41.0 /
+// 33.9 / [33.7] / 33.8.
 constexpr int kOut = 4, kWarps = 8, kThreads = kWarps * 32;
 
 // 16 bytes as pairs
@@ -30,28 +31,19 @@ __device__ __forceinline__ void widen(const uint4& raw, float2 (&v)[VE / 2]) {
     for (int i = 0; i < VE / 2; ++i) v[i] = __bfloat1622float2(h[i]);
   }
 }
-// VE elements of a row from k on as pairs; past K: zeros
-template <typename T, int VE, bool WIDE>
-__device__ __forceinline__ void load_pairs(const T* row, int k, int K, float2 (&v)[VE / 2]) {
-  if (WIDE && k + VE <= K) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < VE / 4; ++i) {
-        const float4 f = *reinterpret_cast<const float4*>(row + k + 4 * i);
-        v[2 * i] = make_float2(f.x, f.y);
-        v[2 * i + 1] = make_float2(f.z, f.w);
-      }
-    } else {
-      uint32_t raw[VE / 2];
-      if constexpr (VE == 8) *reinterpret_cast<uint4*>(raw) = *reinterpret_cast<const uint4*>(row + k);
-      else *reinterpret_cast<uint2*>(raw) = *reinterpret_cast<const uint2*>(row + k);
-#pragma unroll
-      for (int i = 0; i < VE / 2; ++i) v[i] = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw[i]));
+// Four elements of a row from k on as pairs; past K: zeros.  WIDE: bf16 whose rows and length allow 8-byte accesses.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_pairs(const T* row, int k, int K, float2 (&v)[2]) {
+  if constexpr (WIDE) {
+    if (k + 4 <= K) {
+      const uint2 raw = *reinterpret_cast<const uint2*>(row + k);
+      v[0] = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.x));
+      v[1] = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.y));
+      return;
     }
-    return;
   }
 #pragma unroll
-  for (int i = 0; i < VE / 2; ++i) {
+  for (int i = 0; i < 2; ++i) {
     v[i].x = k + 2 * i < K ? (float)row[k + 2 * i] : 0.f;
     v[i].y = k + 2 * i + 1 < K ? (float)row[k + 2 * i + 1] : 0.f;
   }
@@ -150,11 +142,11 @@ __global__ void __launch_bounds__(kThreads, 2) linear_rows_kernel(const LinearPa
     for (int k = (part * 32 + lane) * VE; k < p.k; k += k_warps * 32 * VE) {
       float2 a[kOut][VE / 2];
 #pragma unroll
-      for (int j = 0; j < kOut; ++j) load_pairs<T, VE, false>(w[j], k, p.k, a[j]);
+      for (int j = 0; j < kOut; ++j) load_pairs<false>(w[j], k, p.k, a[j]);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         float2 b[VE / 2];
-        load_pairs<T, VE, false>(x[i], k, p.k, b);
+        load_pairs<false>(x[i], k, p.k, b);
 #pragma unroll
         for (int j = 0; j < kOut; ++j) multiply(a[j], b, i * kOut + j);
       }
@@ -234,7 +226,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) linear_tile_kernel(const Line
         cp_async_16(smem_u32(dst + r * kPitch + kk), k < k1 ? row + k : row, k < k1 ? 16u : 0u);      // (k, k1: multiples of 4)
       } else {
         float2 h[2];
-        load_pairs<T, 4, WIDE>(row, k, k1, h);
+        load_pairs<WIDE>(row, k, k1, h);
         v[i] = make_float4(h[0].x, h[0].y, h[1].x, h[1].y);
       }
     }
@@ -391,11 +383,12 @@ cudaError_t launch_linear_simt(const LinearParams& p, bool bf16, cudaStream_t st
 using namespace dare;
 
 namespace {
-// bf16, up to four rows, of a W that is not large: CUDA cores / tensor cores, us, one row of 1024 x 1000 2.2 / 3.7, 8192 x 1024 5.1 / 7.8
-// (four 6.7 / 7.8), 4096 x 4096 8.7 / 9.9 (two 9.8 / 9.8, three 11.5 / 9.9), 4096 x 6144 13.0 / 12.1, 4096 x 12288 25.9 / 18.7.
+// bf16, up to four rows, of a W that is not large: CUDA cores / tensor cores, W from the HBM, us: one row of 1024 x 1000 2.4 / 3.9, 8192 x 1024
+// 5.3 / 7.6 (four 6.3 / 7.7), 4096 x 4096 8.4 / 9.5 (two 8.9 / 9.6), 4096 x 5000 11.4 / 10.4 (two 12.2 / 10.5), 4096 x 6144 12.4 / 11.9,
+// 4096 x 12288 23.8 / 18.9; three of 4096 x 3000 10.3 / 8.6, four of 4096 x 2560 10.1 / 7.6.
 bool rows_on_cuda_cores(const LinearParams& p) {
   const long long size = (long long)p.n * p.k;
-  return (p.rows <= 2 && size <= 20 << 20) || (p.rows <= 4 && size <= 12 << 20);
+  return (p.rows <= 2 && size <= 18 << 20) || (p.rows <= 4 && size <= 9 << 20);
 }
 }  // namespace
 
