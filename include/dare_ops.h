@@ -7,7 +7,7 @@
  *
  * Conventions of dare.h: plain C, device pointers, dare_status_t, work is enqueued on the given stream and the call returns;
  * nothing is allocated; calls may be captured into a CUDA graph (once a call of the same types has run outside a capture).
- * Strides are in elements, not negative; the elements of a row (of a head) lie side by side.  Rows of an input may overlap or repeat
+ * Strides are in elements, not negative, below 2^38; the elements of a row (of a head) lie side by side.  Rows of an input may overlap or repeat
  * (stride 0), places of an output may not.  Unlike weights of a layer handle, every
  * operand may be what the kernel before on the stream writes.  Outputs must not overlap inputs, except where it is said.
  *

@@ -30,7 +30,7 @@ bool shape_ok(const dare_attention_config_t* c) {
   if (c->q_rows * c->n_heads >= (int64_t)1 << 31) return false;           // (grids and row numbers stay within 31 bits)
   const int64_t s[8] = {c->q_token, c->q_head, c->k_token, c->k_head, c->v_token, c->v_head, c->o_token, c->o_head};
   for (int64_t v : s)
-    if (v < 0 || v >= (int64_t)1 << 38) return false;
+    if (!stride_ok(v)) return false;
   return places_apart(c->q_rows, c->o_token, c->n_heads, c->o_head, c->head_dim);
 }
 bool tc_types(const dare_attention_config_t* c) { return c->dtype == DARE_BF16 && (c->head_dim == 64 || c->head_dim == 128); }

@@ -400,8 +400,7 @@ extern "C" dare_status_t dare_linear(const dare_linear_config_t* c, const void* 
   if (c->rows < 0 || c->rows > (int64_t)1 << 24 || c->in_features <= 0 || c->in_features > 1 << 20 || c->out_features <= 0 ||
       c->out_features > 1 << 24 || c->rows * c->out_features > (int64_t)1 << 38)
     return DARE_ERR_SHAPE;
-  if (c->x_row < 0 || c->w_row < 0 || c->resid_row < 0 || c->y_row < 0 || c->x_row >= (int64_t)1 << 38 || c->w_row >= (int64_t)1 << 38)
-    return DARE_ERR_SHAPE;
+  if (!stride_ok(c->x_row) || !stride_ok(c->w_row) || !stride_ok(c->resid_row) || !stride_ok(c->y_row)) return DARE_ERR_SHAPE;
   if (c->rows > 1 && c->y_row < c->out_features) return DARE_ERR_SHAPE;        // (rows of y in one place would be written twice)
   if (c->rows == 0) return DARE_OK;
   if (!x || !w || !y) return DARE_ERR_INVALID_ARG;

@@ -11,6 +11,10 @@
 
 namespace dare {
 
+// Strides that no memory reaches are refused: their products with counts stay inside 64 bits.
+constexpr long long kMaxStride = 1ll << 38;
+inline bool stride_ok(long long s) { return s >= 0 && s < kMaxStride; }
+
 // Rows (stride `row`) of heads (stride `head`) of `width` elements, written by a launch: no two in one place.
 inline bool places_apart(long long rows, long long row, long long heads, long long head, long long width) {
   if (rows <= 1) return heads <= 1 || head >= width;

@@ -292,7 +292,7 @@ dare_status_t dare_rope(const dare_rope_apply_t* c, const void* x, const int32_t
   if (c->table_positions < 0) return DARE_ERR_SHAPE;
   if (c->tokens == 0 || c->heads == 0) return DARE_OK;
   if (!x || !y || !table) return DARE_ERR_INVALID_ARG;
-  if (c->x_token < 0 || c->x_head < 0 || c->y_token < 0 || c->y_head < 0) return DARE_ERR_SHAPE;
+  if (!stride_ok(c->x_token) || !stride_ok(c->x_head) || !stride_ok(c->y_token) || !stride_ok(c->y_head)) return DARE_ERR_SHAPE;
   if (!places_apart(c->tokens, c->y_token, c->heads, c->y_head, c->head_dim)) return DARE_ERR_SHAPE;
   if (x == y && ((c->tokens > 1 && c->x_token != c->y_token) || (c->heads > 1 && c->x_head != c->y_head))) return DARE_ERR_INVALID_ARG;
   const uintptr_t mask = c->dtype == DARE_BF16 ? 1u : 3u;

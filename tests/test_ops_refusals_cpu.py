@@ -110,3 +110,14 @@ def test_status_off_its_grid(dare):
     ac = dare.AttentionConfig(C.sizeof(dare.AttentionConfig), dare.BF16, 2, 8, 2, 128, 1, 0.1, 16, 64, 1024, 128, 256, 128, 256, 128, 1024, 128)
     need = dare.dare_attention_workspace_bytes(ac)
     assert dare.dare_attention(ac, P, Q, R, S, S + 64, None, 0x50000, None, 0x900000, need, S + 2) == dare.ERR_ALIGN
+
+
+def test_strides_past_any_memory(dare):
+    """Products of a stride and a count have to stay inside 64 bits."""
+    ap = dare.RopeApply(C.sizeof(dare.RopeApply), dare.BF16, 4, 8, 64, 64, 0, 0, 0, 128, 64, 512, 64, 16)
+    for kw in (dict(y_token=1 << 62), dict(y_head=1 << 62), dict(x_token=1 << 62), dict(x_head=1 << 62), dict(y_token=1 << 38),
+               dict(y_token=1 << 61, y_head=1 << 60)):
+        assert dare.dare_rope(_with(ap, **kw), P, None, Q, R) == dare.ERR_SHAPE, kw
+    lc = dare.LinearConfig(C.sizeof(dare.LinearConfig), dare.BF16, 4, 64, 32, 0, 0, 64, 64, 32, 32)
+    for kw in (dict(y_row=1 << 62), dict(resid_row=1 << 62), dict(y_row=1 << 38), dict(resid_row=1 << 38)):
+        assert dare.dare_linear(_with(lc, **kw), P, Q, None, S, R) == dare.ERR_SHAPE, kw
