@@ -410,6 +410,14 @@ def _same_device(index, *tensors):
     return index >= 0
 
 
+def _status_ptr(status):
+    if status is None:
+        return None
+    if status.dtype != _torch.int32 or status.numel() < 1:
+        raise ValueError("status: int32 tensor of one element expected")
+    return status.data_ptr()
+
+
 def _call(fn, name, index, *args):
     """fn(*args, stream) with the tensors' device current."""
     if _device_now() == index:
@@ -469,7 +477,7 @@ def rope(x, table, positions=None, layout=ROPE_LAYOUT["half"], transpose=False, 
     cfg = _ROPE_APPLY.pack(_ROPE_APPLY.size, dt, tokens, heads, hd, 2 * pairs, layout, 1 if transpose else 0, pos_begin, xt, xh, yt,
                            yh, rows)
     _call(_fast_rope, "dare_rope", index, cfg, x.data_ptr(), pos, table.data_ptr(), out.data_ptr(),
-          None if status is None else status.data_ptr())
+          _status_ptr(status))
     return out
 
 
@@ -510,7 +518,7 @@ def linear(x, w, bias=None, act=ACT["none"], resid=None, out=None, status=None):
         raise ValueError("the elements of a row have to lie side by side")
     cfg = _LINEAR.pack(_LINEAR.size, dt, m, k, n, act, 0, xr, wr, rr, yr)
     _call(_fast_linear, "dare_linear", index, cfg, x2.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
-          None if r2 is None else r2.data_ptr(), y2.data_ptr(), None if status is None else status.data_ptr())
+          None if r2 is None else r2.data_ptr(), y2.data_ptr(), _status_ptr(status))
     return out
 
 
@@ -556,7 +564,7 @@ def attention(q, k, v, q_begin, k_begin, k_len=None, causal=False, scale=None, o
     lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device) if return_lse else None
     _call(_fast_attention, "dare_attention", index, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_begin.data_ptr(),
           k_begin.data_ptr(), None if k_len is None else k_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-          work.data_ptr(), nbytes, None if status is None else status.data_ptr())
+          work.data_ptr(), nbytes, _status_ptr(status))
     return (out, lse) if return_lse else out
 
 
