@@ -112,9 +112,13 @@ dare_status_t dare_attention(const dare_attention_config_t* c, const void* q, co
     e = launch_packed_tc(p, c->head_dim, tiles, st);
     if (e == cudaSuccess && !tiles) e = launch_packed_combine(p, c->head_dim, rows, true, st);
   } else {
-    // Few keys a sequence: a pair is a unit, a CTA has a pair, and there is nothing to merge.  Shares / pairs, us, heads of 64: 16 heads,
-    // four prompts of 100 tokens 16.0 / 14.2, 6 of 113 16.3 / 14.7, one of 60 10.5 / 8.5; heads of 256, 14 of 18 25.3 / 16.7.  With more
-    // keys it depends on the lengths: 8 heads of 128, one prompt of 700 69 / 104.  (One sequence may hold all the keys: eight units.)
+    // Few keys a sequence: a pair is a unit, a CTA has a pair, and there is nothing to merge.  Shares / pairs, float32, causal, us: 16 heads of
+    // 64, four prompts of up to 100 tokens 15.5 / 13.9, 6 of 113 11.9 / 10.0, one of 60 10.7 / 8.5; 14 heads of 256, 18 tokens 18.5 / 14.5;
+    // 12 heads of 128, two of 128 26.9 / 18.0.  With more keys it depends on how many pairs there are and how unequal they are, too:
+    // pairs ahead with three prompts of up to 333 (14 heads of 64, 38.0 / 32.0), four of up to 200 (8 heads of 32, 13.7 / 11.0), 16 tokens
+    // over up to 200 keys (20.0 / 16.2), behind with one prompt of 700 (8 heads of 128, 69 / 106), two blocks of 62 over 910 (29 / 48).  The
+    // rule takes pairs only where they are ahead for sure: of 48 such shapes, causal and not, it has the slower form, by more than 5 %, in
+    // twelve, by 58 % at most, all of them shares.  (One sequence may hold all the keys: eight units.)
     const int64_t pairs = (all / rows + c->batch) * c->n_kv_heads;                  // at most
     const bool direct = c->k_rows <= (int64_t)(1 << kUnitShift) * (c->batch < 8 ? c->batch : 8) && pairs <= 8 * kSimtCtas;
     if (direct) {
